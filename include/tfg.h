@@ -84,6 +84,11 @@ typedef enum { TFG_I32 = 0, TFG_I64 = 1 } tfg_index_type;
  * call takes a transposed graph too, that graph's order (edges grouped by
  * source; see tfg_graph_create_transposed). */
 typedef enum { TFG_COO = 0, TFG_CSR = 1, TFG_CSR_T = 2 } tfg_edge_order;
+/* Type of the features, weights and gradients of the graph-transformer layer
+ * (tfg_embedding, tfg_group_norm, tfg_graph_attention): float32 or bfloat16.
+ * Sums, statistics and softmax states are float32 or wider for both. */
+typedef enum { TFG_F32 = 0, TFG_BF16 = 1 } tfg_float_type;
+typedef enum { TFG_ACT_NONE = 0, TFG_ACT_RELU = 1, TFG_ACT_SILU = 2, TFG_ACT_GELU = 3 } tfg_activation;
 
 typedef void *tfg_stream_t; /* hipStream_t */
 
@@ -524,6 +529,135 @@ int tfg_batch_graphs(int64_t G, const void *node_counts, const void *edge_counts
                      void *out_edge_index, void *out_graph_index, int32_t *out_node_offsets,
                      int32_t *out_edge_offsets, int validate, void *ws, size_t ws_bytes,
                      tfg_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Graph-transformer layer over a BatchGraph                                 */
+/* ------------------------------------------------------------------------ */
+/*
+ * Dense counterparts of the edge-wise attention for models that attend between
+ * all nodes of a graph (the Transformer's attention that the paper's library
+ * follows, Sec. 4.2, with every graph of a BatchGraph, Sec. 2.1.1, as its own
+ * sequence): a table lookup for categorical node features, attention inside each
+ * graph, a group norm per graph, and their gradients.
+ * Features, parameters and their gradients are of one float_type (float32 or
+ * bfloat16), rounded once when they are written; sums, statistics and the
+ * softmax are float32 or wider. Gradients overwrite their outputs. Outputs are
+ * dense. Index and offset errors are handled as in tfg_segment_pool: validate !=
+ * 0 waits for the stream and reports them, validate == 0 does not wait (no fault,
+ * unspecified values). Nothing else synchronises or allocates: the calls may be
+ * captured. A workspace belongs to one call at a time (captured graphs that may run
+ * at once need one each).
+ */
+
+/*
+ * Embedding lookup: out[n] = scale * table[ids[n]] ([N, F]); rows whose id is
+ * padding_id are zero. table: [V, F] with leading dimension ldt; ids: [N]
+ * (index_type); padding_id: -1 (none) or an id in [0, V). ws: read only with
+ * validate != 0, tfg_embedding_ws_bytes() bytes (may be NULL otherwise).
+ * Errors: TFG_ERR_INDEX_RANGE (validate: an id outside [0, V); such rows get
+ * unspecified values otherwise), TFG_ERR_INVALID_ARG, TFG_ERR_TOO_LARGE.
+ *
+ * Its gradient: dtable[v] = scale * sum of dout[n] over the n with ids[n] = v
+ * ([V, F] of dout's type, rows without ids and the padding's zero). dout: [N, F]
+ * contiguous. The ids are sorted and every row's terms added in the order of n in
+ * float32, in runs of at most 64 whose sums are joined in order: reproducible bit
+ * for bit. An id outside [0, V) counts as id 0 (validate reports it).
+ */
+size_t tfg_embedding_ws_bytes(void);
+int tfg_embedding(const void *table, int float_type, int64_t V, int64_t F, int64_t ldt,
+                  const void *ids, int index_type, int64_t N, float scale, int64_t padding_id,
+                  void *out, int validate, void *ws, size_t ws_bytes, tfg_stream_t stream);
+size_t tfg_embedding_backward_ws_bytes(int64_t N, int64_t V, int64_t F);
+int tfg_embedding_backward(const void *dout, int float_type, int64_t F, const void *ids,
+                           int index_type, int64_t N, int64_t V, float scale, int64_t padding_id,
+                           void *dtable, int validate, void *ws, size_t ws_bytes,
+                           tfg_stream_t stream);
+
+/*
+ * Group norm with an activation over the graphs of a BatchGraph, channels last:
+ * for graph g and group k of C = F / groups channels, over the graph's nodes and
+ * the group's channels,
+ *   mean, var = their mean and (biased) variance, rstd = 1 / sqrt(var + eps),
+ *   out[n, c] = act(((x[n, c] - mean) * rstd) * gamma[c] + beta[c])
+ * groups = F is an instance norm per graph, groups = 1 a layer norm over the whole
+ * graph. act: TFG_ACT_NONE, _RELU, _SILU (z / (1 + exp(-z))) or _GELU (z * Phi(z),
+ * by erf). x: [Nb, F] with leading dimension ldx; graph_index: [Nb] as in
+ * tfg_segment_pool (a node outside every graph gets unspecified values); gamma,
+ * beta: [F] of the features' type or NULL (ones, zeros); mean, rstd: [G, groups]
+ * float32 (0 for a graph without nodes). Sums are double.
+ *
+ * Its gradient, from dout ([Nb, F], contiguous) and the forward's mean and rstd: with
+ * dz = dout * act'(z), xh = (x - mean) * rstd and dh = dz * gamma,
+ *   dx = rstd * (dh - mean(dh) - xh * mean(dh * xh)) over the same sets,
+ *   dgamma[c] = sum of dz * xh, dbeta[c] = sum of dz over all nodes;
+ * dgamma, dbeta: [F] or NULL. ReLU'(0) = 0.
+ */
+size_t tfg_group_norm_ws_bytes(int64_t Nb, int64_t F, int64_t G, int64_t groups);
+int tfg_group_norm(const void *x, int float_type, int64_t Nb, int64_t F, int64_t ldx,
+                   const void *graph_index, int index_type, int64_t G, int64_t groups,
+                   const void *gamma, const void *beta, float eps, int activation, void *out,
+                   float *mean, float *rstd, int validate, void *ws, size_t ws_bytes,
+                   tfg_stream_t stream);
+size_t tfg_group_norm_backward_ws_bytes(int64_t Nb, int64_t F, int64_t G, int64_t groups);
+int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int64_t Nb, int64_t F,
+                            int64_t ldx, const void *graph_index, int index_type, int64_t G,
+                            int64_t groups, const float *mean, const float *rstd,
+                            const void *gamma, const void *beta, int activation, void *dx,
+                            void *dgamma, void *dbeta, int validate, void *ws, size_t ws_bytes,
+                            tfg_stream_t stream);
+
+/*
+ * Attention inside each graph. Graph g's queries are the rows q_offsets[g] ..
+ * q_offsets[g + 1] - 1 of q, its keys and values the rows k_offsets[g] ..
+ * k_offsets[g + 1] - 1 of k and v ([G + 1] int32, non-decreasing, as
+ * tfg_batch_graphs writes its node offsets; self-attention passes one array
+ * twice, a readout a few queries per graph). For query i, key j of one graph and
+ * head h, whose key/value head is h / (H / kv_heads):
+ *   s = scale * <q[i, h], k[j]>,  t = cap * tanh(s / cap)  (cap = 0: t = s),
+ *   u = t + bias[h, d_ij],
+ *   out[i, h] = sum over j of softmax_j(u) * v[j]
+ * bias: NULL (B = 0), or [H, B] of the features' type, B <= 255, with distance the
+ * pairs' buckets d_ij (hops, say) in bytes: graph g's [queries, keys] row-major from
+ * distance[distance_offsets[g]] on ([G] int64; distance_bytes the array's
+ * length). A pair whose bucket is not below B is masked, and so is one with a
+ * bias of -inf. A query without an unmasked key gets zeros, and lse = -inf.
+ * Values of masked pairs' keys are never part of a score; v is weighted by 0
+ * there, so that a non-finite v does reach the other rows of its graph and head.
+ * q: [Nq, H*D] with leading dimension ldq; k, v: [Nk, kv_heads*D] with ldk, ldv
+ * (columns of one projection may be passed in place); D <= 128, H <= 1024, H /
+ * kv_heads * B <= 4096. out: [Nq, H*D]; lse: NULL or [Nq, H] float32, log of the sum of
+ * exp(u). Rows outside every graph are left as they were.
+ * Where there are few queries and many keys, the keys are split over blocks and
+ * the parts joined in order.
+ * Errors (validate): TFG_ERR_INDEX_RANGE for an offset outside [0, N] or distances
+ * outside their array, TFG_ERR_UNSORTED for decreasing offsets.
+ *
+ * Its gradient, from dout ([Nq, H*D]) and the forward's out and lse (all
+ * contiguous): dq [Nq, H*D], dk, dv [Nk, kv_heads*D] (summed over the heads that
+ * share them), dbias NULL or [H, B]. The softmax's weights are formed again from
+ * lse. bf16: the weights and their gradients are rounded to bf16 as operands of the
+ * products, sums are float32.
+ */
+size_t tfg_graph_attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t kv_heads,
+                                    int64_t D);
+int tfg_graph_attention(const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v,
+                        int64_t ldv, int float_type, int64_t Nq, int64_t Nk,
+                        const int32_t *q_offsets, const int32_t *k_offsets, int64_t G, int64_t H,
+                        int64_t kv_heads, int64_t D, float scale, float cap, const void *bias,
+                        int64_t B, const uint8_t *distance, int64_t distance_bytes,
+                        const int64_t *distance_offsets, void *out, float *lse, int validate,
+                        void *ws, size_t ws_bytes, tfg_stream_t stream);
+size_t tfg_graph_attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H,
+                                             int64_t kv_heads, int64_t D, int64_t B);
+int tfg_graph_attention_backward(const void *dout, const void *q, int64_t ldq, const void *k,
+                                 int64_t ldk, const void *v, int64_t ldv, const void *out,
+                                 const float *lse, int float_type, int64_t Nq, int64_t Nk,
+                                 const int32_t *q_offsets, const int32_t *k_offsets, int64_t G,
+                                 int64_t H, int64_t kv_heads, int64_t D, float scale, float cap,
+                                 const void *bias, int64_t B, const uint8_t *distance,
+                                 int64_t distance_bytes, const int64_t *distance_offsets, void *dq,
+                                 void *dk, void *dv, void *dbias, int validate, void *ws,
+                                 size_t ws_bytes, tfg_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -6,7 +6,8 @@ point of the same name in ``include/tfg.h`` on torch's current stream. All
 computation happens in the HIP kernels of the library; there is no fallback.
 
 Index tensors may be int32 or int64. Features, weights and scores are
-float32. ``edge_index`` has shape [2, E] (row 0 sources, row 1 targets).
+float32 (the graph-transformer layer, ``tfg_embedding``, ``tfg_group_norm`` and
+``tfg_graph_attention``, takes bfloat16 too). ``edge_index`` has shape [2, E] (row 0 sources, row 1 targets).
 """
 
 from __future__ import annotations
@@ -27,6 +28,8 @@ __all__ = [
     "tfg_batch_graphs", "tfg_batch_graphs_totals", "tfg_propagate", "tfg_gat_aggregate",
     "tfg_edge_dot_scores", "tfg_gat_dot_aggregate",
     "tfg_gat_graph_scores", "tfg_segment_softmax_graph", "tfg_segment_softmax_graph_backward",
+    "tfg_embedding", "tfg_embedding_backward", "tfg_group_norm", "tfg_group_norm_backward",
+    "tfg_graph_attention", "tfg_graph_attention_backward",
     "library_path", "load",
 ]
 
@@ -37,6 +40,8 @@ TFG_OK, TFG_ERR_INVALID_ARG, TFG_ERR_INDEX_RANGE, TFG_ERR_UNSORTED = 0, 1, 2, 3
 TFG_ERR_TOO_LARGE, TFG_ERR_WORKSPACE, TFG_ERR_HIP = 4, 5, 6
 _REDUCE = {"sum": 0, "mean": 1, "max": 2}
 _ORDER = {"coo": 0, "csr": 1, "csr_t": 2}
+_FLOAT = {torch.float32: 0, torch.bfloat16: 1}
+_ACTIVATION = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 _lib = None
 
@@ -122,6 +127,26 @@ def load():
         "tfg_segment_softmax_graph_ws_bytes": (sz, [p, i64]),
         "tfg_segment_softmax_graph": (ci, [p, p, i64, ci, p, p, sz, p]),
         "tfg_segment_softmax_graph_backward": (ci, [p, p, p, i64, ci, p, p, sz, p]),
+        "tfg_embedding_ws_bytes": (sz, []),
+        "tfg_embedding": (ci, [p, ci, i64, i64, i64, p, ci, i64, ctypes.c_float, i64, p, ci, p, sz,
+                               p]),
+        "tfg_embedding_backward_ws_bytes": (sz, [i64, i64, i64]),
+        "tfg_embedding_backward": (ci, [p, ci, i64, p, ci, i64, i64, ctypes.c_float, i64, p, ci, p,
+                                        sz, p]),
+        "tfg_group_norm_ws_bytes": (sz, [i64] * 4),
+        "tfg_group_norm": (ci, [p, ci, i64, i64, i64, p, ci, i64, i64, p, p, ctypes.c_float, ci, p,
+                                p, p, ci, p, sz, p]),
+        "tfg_group_norm_backward_ws_bytes": (sz, [i64] * 4),
+        "tfg_group_norm_backward": (ci, [p, p, ci, i64, i64, i64, p, ci, i64, i64, p, p, p, p, ci,
+                                         p, p, p, ci, p, sz, p]),
+        "tfg_graph_attention_ws_bytes": (sz, [i64] * 6),
+        "tfg_graph_attention": (ci, [p, i64, p, i64, p, i64, ci, i64, i64, p, p, i64, i64, i64, i64,
+                                     ctypes.c_float, ctypes.c_float, p, i64, p, i64, p, p, p, ci,
+                                     p, sz, p]),
+        "tfg_graph_attention_backward_ws_bytes": (sz, [i64] * 7),
+        "tfg_graph_attention_backward": (ci, [p, p, i64, p, i64, p, i64, p, p, ci, i64, i64, p, p,
+                                              i64, i64, i64, i64, ctypes.c_float, ctypes.c_float,
+                                              p, i64, p, i64, p, p, p, p, p, ci, p, sz, p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -880,3 +905,284 @@ def tfg_gat_dot_aggregate(graph: Graph, q: torch.Tensor, key: torch.Tensor, v: t
                                      float(scale), _ptr(out), _ptr(alpha), _ptr(ws), _nbytes(ws),
                                      _stream(dev)))
     return (out, alpha) if want_alpha else out
+
+
+def _float_type(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _FLOAT:
+        raise TypeError(f"{what} must be float32 or bfloat16, got {t.dtype}")
+    return _FLOAT[t.dtype]
+
+
+def _typed(t: torch.Tensor, like: torch.Tensor, shape, what: str) -> torch.Tensor:
+    """A contiguous input of the device and dtype of `like` and of exactly `shape`."""
+    _dev(t, what, like.device)
+    if t.dtype != like.dtype:
+        raise TypeError(f"{what} must be {like.dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t.contiguous()
+
+
+def _matrix(x: torch.Tensor, what: str, like: torch.Tensor | None = None):
+    """A float32 or bfloat16 device matrix with unit column stride; (x, ldx)."""
+    _dev(x, what, like.device if like is not None else None)
+    _float_type(x, what)
+    if like is not None and x.dtype != like.dtype:
+        raise TypeError(f"{what} must be {like.dtype}, got {x.dtype}")
+    if x.dim() != 2:
+        raise ValueError(f"{what} must be a matrix")
+    if (x.stride(1) != 1 and x.shape[1] > 1) or (x.stride(0) < x.shape[1] and x.shape[0] > 1):
+        x = x.contiguous()
+    return x, max(x.stride(0), x.shape[1])
+
+
+def _ids(t: torch.Tensor, what: str, device) -> torch.Tensor:
+    _dev(t, what, device)
+    _index_type(t)
+    if t.dim() != 1:
+        raise ValueError(f"{what} must be one-dimensional")
+    return t.contiguous()
+
+
+def _offsets(t: torch.Tensor, what: str, device, dtype=torch.int32) -> torch.Tensor:
+    _dev(t, what, device)
+    if t.dtype != dtype or t.dim() != 1:
+        raise TypeError(f"{what} must be a one-dimensional {dtype} tensor")
+    return t.contiguous()
+
+
+def tfg_embedding(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+                  padding_id: int | None = None, validate: bool = True,
+                  out: torch.Tensor | None = None) -> torch.Tensor:
+    """scale * table[ids]: rows [N, F] of table [V, F] (float32 or bfloat16) by ids
+    [N]; rows whose id is ``padding_id`` are zero."""
+    lib = load()
+    table, ldt = _matrix(table, "table")
+    dev = table.device
+    ids = _ids(ids, "ids", dev)
+    V, F = table.shape
+    N = ids.shape[0]
+    if padding_id is not None and not 0 <= padding_id < V:
+        raise ValueError("padding_id must lie in [0, V)")
+    if out is None:
+        out = torch.empty((N, F), dtype=table.dtype, device=dev)
+    _out(out, (N, F), table.dtype, dev, "out")
+    with torch.cuda.device(dev):
+        ws = _workspace(lib.tfg_embedding_ws_bytes(), dev) if validate else None
+        _check(lib.tfg_embedding(_ptr(table), _float_type(table, "table"), V, F, ldt, _ptr(ids),
+                                 _index_type(ids), N, float(scale),
+                                 -1 if padding_id is None else padding_id, _ptr(out), int(validate),
+                                 _ptr(ws), _nbytes(ws) if validate else 0, _stream(dev)))
+    return out
+
+
+def tfg_embedding_backward(dout: torch.Tensor, ids: torch.Tensor, V: int, scale: float = 1.0,
+                           padding_id: int | None = None, validate: bool = True,
+                           out: torch.Tensor | None = None,
+                           ws: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of ``tfg_embedding`` with respect to the table: [V, F] of dout's type,
+    for dout = dL/d out [N, F]; every row's terms are added in the order of n."""
+    lib = load()
+    dout, _ = _matrix(dout, "dout")
+    dout = dout.contiguous()
+    dev = dout.device
+    ids = _ids(ids, "ids", dev)
+    N, F = dout.shape
+    if ids.shape[0] != N:
+        raise ValueError("ids must hold one id per row of dout")
+    if padding_id is not None and not 0 <= padding_id < V:
+        raise ValueError("padding_id must lie in [0, V)")
+    if out is None:
+        out = torch.empty((V, F), dtype=dout.dtype, device=dev)
+    _out(out, (V, F), dout.dtype, dev, "out")
+    with torch.cuda.device(dev):
+        ws = _ws(ws, lib.tfg_embedding_backward_ws_bytes(N, V, F), dev)
+        _check(lib.tfg_embedding_backward(_ptr(dout), _float_type(dout, "dout"), F, _ptr(ids),
+                                          _index_type(ids), N, V, float(scale),
+                                          -1 if padding_id is None else padding_id, _ptr(out),
+                                          int(validate), _ptr(ws), _nbytes(ws), _stream(dev)))
+    return out
+
+
+def tfg_group_norm(x: torch.Tensor, graph_index: torch.Tensor, G: int, groups: int,
+                   gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None,
+                   eps: float = 1e-5, activation: str = "none", validate: bool = True,
+                   out: torch.Tensor | None = None, ws: torch.Tensor | None = None):
+    """Group norm with an activation ("none", "relu", "silu", "gelu") over each graph of
+    a BatchGraph: x [Nb, F], channels last, in ``groups`` groups. Returns (out [Nb, F],
+    mean, rstd [G, groups] float32)."""
+    lib = load()
+    x, ldx = _matrix(x, "x")
+    dev = x.device
+    gi = _ids(graph_index, "graph_index", dev)
+    Nb, F = x.shape
+    if gi.shape[0] != Nb:
+        raise ValueError("graph_index must hold one graph id per node")
+    gamma = None if gamma is None else _typed(gamma, x, (F,), "gamma")
+    beta = None if beta is None else _typed(beta, x, (F,), "beta")
+    if out is None:
+        out = torch.empty((Nb, F), dtype=x.dtype, device=dev)
+    _out(out, (Nb, F), x.dtype, dev, "out")
+    mean = torch.empty((G, groups), dtype=torch.float32, device=dev)
+    rstd = torch.empty_like(mean)
+    with torch.cuda.device(dev):
+        ws = _ws(ws, lib.tfg_group_norm_ws_bytes(Nb, F, G, groups), dev)
+        _check(lib.tfg_group_norm(_ptr(x), _float_type(x, "x"), Nb, F, ldx, _ptr(gi),
+                                  _index_type(gi), G, groups, _ptr(gamma), _ptr(beta), float(eps),
+                                  _ACTIVATION[activation], _ptr(out), _ptr(mean), _ptr(rstd),
+                                  int(validate), _ptr(ws), _nbytes(ws), _stream(dev)))
+    return out, mean, rstd
+
+
+def tfg_group_norm_backward(dout: torch.Tensor, x: torch.Tensor, graph_index: torch.Tensor, G: int,
+                            groups: int, mean: torch.Tensor, rstd: torch.Tensor,
+                            gamma: torch.Tensor | None = None, beta: torch.Tensor | None = None,
+                            activation: str = "none", validate: bool = True,
+                            want_params: bool = True, ws: torch.Tensor | None = None):
+    """Gradients of ``tfg_group_norm`` for dout = dL/d out: (dx [Nb, F], dgamma [F],
+    dbeta [F]); mean and rstd as the forward call returned them. Without
+    ``want_params`` dgamma and dbeta are None."""
+    lib = load()
+    x, ldx = _matrix(x, "x")
+    dev = x.device
+    gi = _ids(graph_index, "graph_index", dev)
+    Nb, F = x.shape
+    if gi.shape[0] != Nb:
+        raise ValueError("graph_index must hold one graph id per node")
+    dout = _typed(dout, x, (Nb, F), "dout")
+    gamma = None if gamma is None else _typed(gamma, x, (F,), "gamma")
+    beta = None if beta is None else _typed(beta, x, (F,), "beta")
+    stats = []
+    for t, what in ((mean, "mean"), (rstd, "rstd")):
+        t = _f32(t, what, dev)
+        if tuple(t.shape) != (G, groups):
+            raise ValueError(f"{what} must be [G, groups]")
+        stats.append(t)
+    dx = torch.empty((Nb, F), dtype=x.dtype, device=dev)
+    dgamma = torch.empty(F, dtype=x.dtype, device=dev) if want_params else None
+    dbeta = torch.empty(F, dtype=x.dtype, device=dev) if want_params else None
+    with torch.cuda.device(dev):
+        ws = _ws(ws, lib.tfg_group_norm_backward_ws_bytes(Nb, F, G, groups), dev)
+        _check(lib.tfg_group_norm_backward(_ptr(dout), _ptr(x), _float_type(x, "x"), Nb, F, ldx,
+                                           _ptr(gi), _index_type(gi), G, groups, _ptr(stats[0]),
+                                           _ptr(stats[1]), _ptr(gamma), _ptr(beta),
+                                           _ACTIVATION[activation], _ptr(dx), _ptr(dgamma),
+                                           _ptr(dbeta), int(validate), _ptr(ws), _nbytes(ws),
+                                           _stream(dev)))
+    return dx, dgamma, dbeta
+
+
+class _Attention:
+    """The checked arguments that both directions of the graph attention share."""
+
+    def __init__(self, q, k, v, q_offsets, k_offsets, heads, kv_heads, scale, cap, bias, distance,
+                 distance_offsets):
+        self.q, self.ldq = _matrix(q, "q")
+        self.k, self.ldk = _matrix(k, "k", self.q)
+        self.v, self.ldv = _matrix(v, "v", self.q)
+        self.dev, self.dtype = self.q.device, self.q.dtype
+        self.H, self.Hk = heads, heads if kv_heads is None else kv_heads
+        if self.H < 1 or self.Hk < 1 or self.H % self.Hk:
+            raise ValueError("heads must be a positive multiple of kv_heads")
+        self.Nq, self.Nk = self.q.shape[0], self.k.shape[0]
+        self.D = self.q.shape[1] // self.H
+        if self.q.shape[1] != self.H * self.D or self.D < 1:
+            raise ValueError("q must be [Nq, heads * D]")
+        if self.k.shape[1] != self.Hk * self.D or self.v.shape != self.k.shape:
+            raise ValueError("k and v must be [Nk, kv_heads * D]")
+        self.qoff = _offsets(q_offsets, "q_offsets", self.dev)
+        self.koff = self.qoff if k_offsets is None else _offsets(k_offsets, "k_offsets", self.dev)
+        self.G = self.qoff.shape[0] - 1
+        if self.G < 0 or self.koff.shape != self.qoff.shape:
+            raise ValueError("q_offsets and k_offsets must be [G + 1]")
+        self.scale = 1.0 / (self.D ** 0.5) if scale is None else float(scale)
+        self.cap = float(cap)
+        self.bias = self.dist = self.doff = None
+        self.B = 0
+        if bias is not None:
+            if distance is None or distance_offsets is None:
+                raise ValueError("a bias needs distance and distance_offsets")
+            if bias.dim() != 2 or not 1 <= bias.shape[1] <= 255:
+                raise ValueError("bias must be [heads, B] with 1 <= B <= 255")
+            self.B = bias.shape[1]
+            self.bias = _typed(bias, self.q, (self.H, self.B), "bias")
+            _dev(distance, "distance", self.dev)
+            if distance.dtype != torch.uint8 or distance.dim() != 1:
+                raise TypeError("distance must be a one-dimensional uint8 tensor")
+            self.dist = distance.contiguous()
+            self.doff = _offsets(distance_offsets, "distance_offsets", self.dev, torch.int64)
+            if self.doff.shape[0] < self.G:
+                raise ValueError("distance_offsets must hold one offset per graph")
+        elif distance is not None:
+            raise ValueError("distance without a bias")
+
+    def inputs(self):
+        return (_ptr(self.q), self.ldq, _ptr(self.k), self.ldk, _ptr(self.v), self.ldv)
+
+    def shape(self):
+        return (self.Nq, self.Nk, _ptr(self.qoff), _ptr(self.koff), self.G, self.H, self.Hk, self.D,
+                self.scale, self.cap, _ptr(self.bias), self.B, _ptr(self.dist),
+                0 if self.dist is None else self.dist.numel(), _ptr(self.doff))
+
+
+def tfg_graph_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                        heads: int, k_offsets: torch.Tensor | None = None,
+                        kv_heads: int | None = None, scale: float | None = None, cap: float = 0.0,
+                        bias: torch.Tensor | None = None, distance: torch.Tensor | None = None,
+                        distance_offsets: torch.Tensor | None = None, validate: bool = True,
+                        want_lse: bool = False, out: torch.Tensor | None = None,
+                        ws: torch.Tensor | None = None):
+    """Attention inside each graph of a BatchGraph: out [Nq, heads*D] (and lse [Nq, heads]
+    with ``want_lse``) for q [Nq, heads*D], k and v [Nk, kv_heads*D] (row strides are
+    free). Graph g's rows are given by the offsets [G + 1] (int32, tfg_batch_graphs'
+    node offsets; k_offsets defaults to q_offsets). ``cap``: scores become cap *
+    tanh(score / cap). ``bias`` [heads, B] is added by each pair's bucket in
+    ``distance`` (uint8; graph g's [queries, keys] from distance_offsets[g] on); a
+    bucket from B on masks the pair. scale defaults to 1/sqrt(D)."""
+    lib = load()
+    a = _Attention(q, k, v, q_offsets, k_offsets, heads, kv_heads, scale, cap, bias, distance,
+                   distance_offsets)
+    if out is None:
+        out = torch.empty((a.Nq, a.H * a.D), dtype=a.dtype, device=a.dev)
+    _out(out, (a.Nq, a.H * a.D), a.dtype, a.dev, "out")
+    lse = torch.empty((a.Nq, a.H), dtype=torch.float32, device=a.dev) if want_lse else None
+    with torch.cuda.device(a.dev):
+        ws = _ws(ws, lib.tfg_graph_attention_ws_bytes(a.Nq, a.Nk, a.G, a.H, a.Hk, a.D), a.dev)
+        _check(lib.tfg_graph_attention(*a.inputs(), _FLOAT[a.dtype], *a.shape(), _ptr(out),
+                                       _ptr(lse), int(validate), _ptr(ws), _nbytes(ws),
+                                       _stream(a.dev)))
+    return (out, lse) if want_lse else out
+
+
+def tfg_graph_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                                 v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                                 q_offsets: torch.Tensor, heads: int,
+                                 k_offsets: torch.Tensor | None = None,
+                                 kv_heads: int | None = None, scale: float | None = None,
+                                 cap: float = 0.0, bias: torch.Tensor | None = None,
+                                 distance: torch.Tensor | None = None,
+                                 distance_offsets: torch.Tensor | None = None,
+                                 validate: bool = True, want_dbias: bool = True,
+                                 ws: torch.Tensor | None = None):
+    """Gradients of ``tfg_graph_attention`` for dout = dL/d out, from the forward's out
+    and lse: (dq [Nq, heads*D], dk, dv [Nk, kv_heads*D], dbias [heads, B] or None)."""
+    lib = load()
+    a = _Attention(q, k, v, q_offsets, k_offsets, heads, kv_heads, scale, cap, bias, distance,
+                   distance_offsets)
+    dout = _typed(dout, a.q, (a.Nq, a.H * a.D), "dout")
+    out = _typed(out, a.q, (a.Nq, a.H * a.D), "out")
+    lse = _f32(lse, "lse", a.dev)
+    if tuple(lse.shape) != (a.Nq, a.H):
+        raise ValueError("lse must be [Nq, heads]")
+    dq = torch.empty((a.Nq, a.H * a.D), dtype=a.dtype, device=a.dev)
+    dk = torch.empty((a.Nk, a.Hk * a.D), dtype=a.dtype, device=a.dev)
+    dv = torch.empty_like(dk)
+    dbias = torch.empty_like(a.bias) if a.B and want_dbias else None
+    with torch.cuda.device(a.dev):
+        ws = _ws(ws, lib.tfg_graph_attention_backward_ws_bytes(a.Nq, a.Nk, a.G, a.H, a.Hk, a.D, a.B),
+                 a.dev)
+        _check(lib.tfg_graph_attention_backward(_ptr(dout), *a.inputs(), _ptr(out), _ptr(lse),
+                                                _FLOAT[a.dtype], *a.shape(), _ptr(dq), _ptr(dk),
+                                                _ptr(dv), _ptr(dbias), int(validate), _ptr(ws),
+                                                _nbytes(ws), _stream(a.dev)))
+    return dq, dk, dv, dbias

@@ -17,7 +17,8 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libtfg.so")
 SOURCES = ["csr.hip", "norm.hip", "aggregate.hip", "slots_sum.hip", "slots_max.hip",
            "slots_heads.hip", "slots_masked.hip", "softmax.hip",
-           "gat.hip", "gat_dot.hip", "pool.hip", "batch.hip", "backward.hip", "api.cpp"]
+           "gat.hip", "gat_dot.hip", "pool.hip", "batch.hip", "backward.hip",
+           "embed.hip", "group_norm.hip", "attention.hip", "attention_grad.hip", "api.cpp"]
 # measurement probes for the benchmark (include/tfg_probe.h), a library of their own
 PROBE_LIB = os.path.join(HERE, "libtfg_probe.so")
 PROBE_SOURCES = ["probe.hip"]

@@ -940,5 +940,284 @@ int tfg_segment_softmax_graph_backward(const tfg_graph* g, const float* alpha,
                                          as_stream(stream), order == TFG_CSR);
 }
 
-}  // extern "C"
+// ---- the graph-transformer layer -----------------------------------------------
 
+namespace {
+
+bool bad_float_type(int t) { return t != TFG_F32 && t != TFG_BF16; }
+
+// The device flag of a validated call, as a status.
+int read_flag(const int* err, hipStream_t s, const char* range, const char* order) {
+  int flags = 0;
+  const int* from[1] = {err};
+  if (int rc = read_back(s, 1, from, &flags)) return rc;
+  if (flags & kErrIndex) return fail(TFG_ERR_INDEX_RANGE, range);
+  if (flags & kErrUnsorted) return fail(TFG_ERR_UNSORTED, order);
+  return TFG_OK;
+}
+
+int check_embedding(const void* ids, int float_type, int index_type, int64_t V, int64_t F,
+                    int64_t N, int64_t padding_id) {
+  if (bad_float_type(float_type)) return fail(TFG_ERR_INVALID_ARG, "bad float type");
+  if (bad_index_type(index_type)) return fail(TFG_ERR_INVALID_ARG, "bad index type");
+  if (int rc = check_counts(0, N, V)) return rc;
+  if (F < 0 || F >= kMaxCount) return fail(TFG_ERR_INVALID_ARG, "bad F");
+  if (padding_id < -1 || padding_id >= V) return fail(TFG_ERR_INVALID_ARG, "padding_id outside [0, V)");
+  if (N > 0 && V == 0) return fail(TFG_ERR_INVALID_ARG, "ids into an empty table");
+  if (N > 0 && F > 0 && ids == nullptr) return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  return TFG_OK;
+}
+
+const char* const kIdRange = "ids holds an id outside [0, V)";
+
+int check_norm(const GroupNorm& n) {
+  if (bad_float_type(n.float_type)) return fail(TFG_ERR_INVALID_ARG, "bad float type");
+  if (bad_index_type(n.index_type)) return fail(TFG_ERR_INVALID_ARG, "bad index type");
+  if (int rc = check_counts(0, n.Nb, 0)) return rc;
+  if (n.G < 0 || n.G >= kMaxCount) return fail(TFG_ERR_INVALID_ARG, "bad G");
+  if (n.F < 0 || n.F >= kMaxCount || n.ldx < n.F) return fail(TFG_ERR_INVALID_ARG, "bad F / ldx");
+  if (n.K < 1 || n.F % n.K != 0) return fail(TFG_ERR_INVALID_ARG, "groups must divide F");
+  if (n.G * n.K >= kMaxCount) return fail(TFG_ERR_TOO_LARGE, "G * groups not below 2^31 - 2^20");
+  if (n.act < TFG_ACT_NONE || n.act > TFG_ACT_GELU) return fail(TFG_ERR_INVALID_ARG, "bad activation");
+  return TFG_OK;
+}
+
+int run_norm(const GroupNorm& n, bool bwd, int validate, void* ws, size_t ws_bytes,
+             tfg_stream_t stream) {
+  if (int wrc = check_ws(ws, ws_bytes, group_norm_ws_bytes(n.Nb, n.F, n.G, n.K, bwd))) return wrc;
+  hipStream_t s = as_stream(stream);
+  int* err = validate ? group_norm_flag(n.G, ws) : nullptr;
+  if (n.F == 0) return TFG_OK;
+  if (int rc = launch_group_norm(n, bwd, ws, err, s)) return rc;
+  return validate ? read_flag(err, s, "graph_index holds an id outside [0, G)",
+                              "graph_index is not non-decreasing") : TFG_OK;
+}
+
+int check_attention(const AttnShape& a, int float_type, int64_t Nq, int64_t Nk, int64_t G, int64_t H,
+                    int64_t Hk, int64_t D, int64_t B) {
+  if (bad_float_type(float_type)) return fail(TFG_ERR_INVALID_ARG, "bad float type");
+  if (int rc = check_counts(0, Nq, Nk)) return rc;
+  if (G < 0 || G >= kMaxCount) return fail(TFG_ERR_INVALID_ARG, "bad G");
+  if (Hk < 1 || H < 1 || H % Hk != 0 || H > 1024)
+    return fail(TFG_ERR_INVALID_ARG, "need 1 <= H <= 1024 and kv_heads dividing H");
+  if (D < 1 || D > max_attention_width()) return fail(TFG_ERR_INVALID_ARG, "need 1 <= D <= 128");
+  if (a.ldq < H * D || a.ldk < Hk * D || a.ldv < Hk * D)
+    return fail(TFG_ERR_INVALID_ARG, "a leading dimension below the row's width");
+  if (!(a.cap >= 0.0f) || a.cap > 3.4e38f) return fail(TFG_ERR_INVALID_ARG, "bad cap");
+  if (B < 0 || B > 255) return fail(TFG_ERR_INVALID_ARG, "need 0 <= B <= 255");
+  if (H / Hk * B > max_attention_bias_entries())
+    return fail(TFG_ERR_INVALID_ARG, "need H / kv_heads * B <= 4096");
+  if (a.dist_bytes < 0) return fail(TFG_ERR_INVALID_ARG, "negative size");
+  if (G > 0 && (a.qoff == nullptr || a.koff == nullptr)) return fail(TFG_ERR_INVALID_ARG, "NULL offsets");
+  if (B > 0 && (a.bias == nullptr || (G > 0 && a.doff == nullptr) || (a.dist_bytes > 0 && a.dist == nullptr)))
+    return fail(TFG_ERR_INVALID_ARG, "a bias needs bias, distance and distance_offsets");
+  return TFG_OK;
+}
+
+AttnShape attention_shape(int64_t ldq, int64_t ldk, int64_t ldv, int64_t Nq, int64_t Nk,
+                          const int32_t* q_offsets, const int32_t* k_offsets, int64_t G, int64_t H,
+                          int64_t Hk, int64_t D, float scale, float cap, const void* bias, int64_t B,
+                          const uint8_t* distance, int64_t distance_bytes,
+                          const int64_t* distance_offsets) {
+  AttnShape a{};
+  a.qoff = q_offsets;
+  a.koff = k_offsets;
+  a.doff = distance_offsets;
+  a.dist = distance;
+  a.dist_bytes = distance_bytes;
+  a.bias = bias;
+  a.B = (int)B;
+  a.Nq = (int)Nq;
+  a.Nk = (int)Nk;
+  a.G = (int)G;
+  a.H = (int)H;
+  a.Hk = (int)Hk;
+  a.D = (int)D;
+  a.scale = scale;
+  a.cap = cap;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  return a;
+}
+
+const char* const kOffRange = "an offset lies outside [0, N], or distances outside their array";
+const char* const kOffOrder = "offsets are not non-decreasing";
+
+}  // namespace
+
+size_t tfg_embedding_ws_bytes(void) { return 256; }
+
+int tfg_embedding(const void *table, int float_type, int64_t V, int64_t F, int64_t ldt,
+                  const void *ids, int index_type, int64_t N, float scale, int64_t padding_id,
+                  void *out, int validate, void *ws, size_t ws_bytes, tfg_stream_t stream) {
+  if (int rc = check_embedding(ids, float_type, index_type, V, F, N, padding_id)) return rc;
+  if (ldt < F) return fail(TFG_ERR_INVALID_ARG, "bad ldt");
+  if (N > 0 && F > 0 && (table == nullptr || out == nullptr))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  if (validate)
+    if (int wrc = check_ws(ws, ws_bytes, tfg_embedding_ws_bytes())) return wrc;
+  hipStream_t s = as_stream(stream);
+  const Embed a{table, ids, out, float_type, index_type, V, F, ldt, N, padding_id, scale};
+  int* err = validate ? static_cast<int*>(ws) : nullptr;
+  if (int rc = launch_embedding(a, err, s)) return rc;
+  return validate ? read_flag(err, s, kIdRange, "") : TFG_OK;
+}
+
+size_t tfg_embedding_backward_ws_bytes(int64_t N, int64_t V, int64_t F) {
+  if (N < 0 || V < 0 || F < 0 || N >= kMaxCount || V >= kMaxCount || F >= kMaxCount) return 0;
+  return embedding_backward_ws_bytes(N, V, F);
+}
+
+int tfg_embedding_backward(const void *dout, int float_type, int64_t F, const void *ids,
+                           int index_type, int64_t N, int64_t V, float scale, int64_t padding_id,
+                           void *dtable, int validate, void *ws, size_t ws_bytes,
+                           tfg_stream_t stream) {
+  if (int rc = check_embedding(ids, float_type, index_type, V, F, N, padding_id)) return rc;
+  if ((N > 0 && F > 0 && dout == nullptr) || (V > 0 && F > 0 && dtable == nullptr))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  if (int wrc = check_ws(ws, ws_bytes, embedding_backward_ws_bytes(N, V, F))) return wrc;
+  hipStream_t s = as_stream(stream);
+  const Embed a{nullptr, ids, nullptr, float_type, index_type, V, F, F, N, padding_id, scale};
+  int* err = validate ? static_cast<int*>(ws) : nullptr;
+  if (int rc = launch_embedding_backward(a, dout, dtable, ws, err, s)) return rc;
+  return validate ? read_flag(err, s, kIdRange, "") : TFG_OK;
+}
+
+size_t tfg_group_norm_ws_bytes(int64_t Nb, int64_t F, int64_t G, int64_t groups) {
+  if (Nb < 0 || F < 0 || G < 0 || groups < 1 || Nb >= kMaxCount || F >= kMaxCount || G >= kMaxCount)
+    return 0;
+  return group_norm_ws_bytes(Nb, F, G, groups, false);
+}
+
+int tfg_group_norm(const void *x, int float_type, int64_t Nb, int64_t F, int64_t ldx,
+                   const void *graph_index, int index_type, int64_t G, int64_t groups,
+                   const void *gamma, const void *beta, float eps, int activation, void *out,
+                   float *mean, float *rstd, int validate, void *ws, size_t ws_bytes,
+                   tfg_stream_t stream) {
+  GroupNorm n{};
+  n.x = x;
+  n.graph_index = graph_index;
+  n.gamma = gamma;
+  n.beta = beta;
+  n.out = out;
+  n.mean = mean;
+  n.rstd = rstd;
+  n.float_type = float_type;
+  n.index_type = index_type;
+  n.act = activation;
+  n.Nb = Nb;
+  n.F = F;
+  n.ldx = ldx;
+  n.G = G;
+  n.K = groups;
+  n.eps = eps;
+  if (int rc = check_norm(n)) return rc;
+  if (!(eps >= 0.0f)) return fail(TFG_ERR_INVALID_ARG, "bad eps");
+  if ((Nb > 0 && F > 0 && (x == nullptr || graph_index == nullptr || out == nullptr)) ||
+      (G > 0 && F > 0 && (mean == nullptr || rstd == nullptr)))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  return run_norm(n, false, validate, ws, ws_bytes, stream);
+}
+
+size_t tfg_group_norm_backward_ws_bytes(int64_t Nb, int64_t F, int64_t G, int64_t groups) {
+  if (Nb < 0 || F < 0 || G < 0 || groups < 1 || Nb >= kMaxCount || F >= kMaxCount || G >= kMaxCount)
+    return 0;
+  return group_norm_ws_bytes(Nb, F, G, groups, true);
+}
+
+int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int64_t Nb, int64_t F,
+                            int64_t ldx, const void *graph_index, int index_type, int64_t G,
+                            int64_t groups, const float *mean, const float *rstd,
+                            const void *gamma, const void *beta, int activation, void *dx,
+                            void *dgamma, void *dbeta, int validate, void *ws, size_t ws_bytes,
+                            tfg_stream_t stream) {
+  GroupNorm n{};
+  n.x = x;
+  n.dout = dout;
+  n.graph_index = graph_index;
+  n.gamma = gamma;
+  n.beta = beta;
+  n.dx = dx;
+  n.dgamma = dgamma;
+  n.dbeta = dbeta;
+  n.mean = const_cast<float*>(mean);  // (read only in this direction)
+  n.rstd = const_cast<float*>(rstd);
+  n.float_type = float_type;
+  n.index_type = index_type;
+  n.act = activation;
+  n.Nb = Nb;
+  n.F = F;
+  n.ldx = ldx;
+  n.G = G;
+  n.K = groups;
+  if (int rc = check_norm(n)) return rc;
+  if ((Nb > 0 && F > 0 && (x == nullptr || dout == nullptr || graph_index == nullptr || dx == nullptr)) ||
+      (G > 0 && F > 0 && (mean == nullptr || rstd == nullptr)))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  return run_norm(n, true, validate, ws, ws_bytes, stream);
+}
+
+size_t tfg_graph_attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t kv_heads,
+                                    int64_t D) {
+  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1) return 0;
+  return 256 + attention_ws_bytes(Nq, Nk, G, H, kv_heads, D);
+}
+
+int tfg_graph_attention(const void *q, int64_t ldq, const void *k, int64_t ldk, const void *v,
+                        int64_t ldv, int float_type, int64_t Nq, int64_t Nk,
+                        const int32_t *q_offsets, const int32_t *k_offsets, int64_t G, int64_t H,
+                        int64_t kv_heads, int64_t D, float scale, float cap, const void *bias,
+                        int64_t B, const uint8_t *distance, int64_t distance_bytes,
+                        const int64_t *distance_offsets, void *out, float *lse, int validate,
+                        void *ws, size_t ws_bytes, tfg_stream_t stream) {
+  const AttnShape a = attention_shape(ldq, ldk, ldv, Nq, Nk, q_offsets, k_offsets, G, H, kv_heads, D,
+                                      scale, cap, bias, B, distance, distance_bytes, distance_offsets);
+  if (int rc = check_attention(a, float_type, Nq, Nk, G, H, kv_heads, D, B)) return rc;
+  if ((Nq > 0 && (q == nullptr || out == nullptr)) || (Nk > 0 && (k == nullptr || v == nullptr)))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  if (int wrc = check_ws(ws, ws_bytes, tfg_graph_attention_ws_bytes(Nq, Nk, G, H, kv_heads, D))) return wrc;
+  hipStream_t s = as_stream(stream);
+  int* err = static_cast<int*>(ws);
+  if (validate && G > 0)
+    if (int rc = launch_attention_check(a, err, s)) return rc;
+  if (int rc = launch_attention(a, float_type, q, k, v, out, lse, static_cast<char*>(ws) + 256, s))
+    return rc;
+  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder) : TFG_OK;
+}
+
+size_t tfg_graph_attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H,
+                                             int64_t kv_heads, int64_t D, int64_t B) {
+  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1 || B < 0) return 0;
+  return 256 + attention_backward_ws_bytes(Nq, G, H, kv_heads, D, B);
+}
+
+int tfg_graph_attention_backward(const void *dout, const void *q, int64_t ldq, const void *k,
+                                 int64_t ldk, const void *v, int64_t ldv, const void *out,
+                                 const float *lse, int float_type, int64_t Nq, int64_t Nk,
+                                 const int32_t *q_offsets, const int32_t *k_offsets, int64_t G,
+                                 int64_t H, int64_t kv_heads, int64_t D, float scale, float cap,
+                                 const void *bias, int64_t B, const uint8_t *distance,
+                                 int64_t distance_bytes, const int64_t *distance_offsets, void *dq,
+                                 void *dk, void *dv, void *dbias, int validate, void *ws,
+                                 size_t ws_bytes, tfg_stream_t stream) {
+  const AttnShape a = attention_shape(ldq, ldk, ldv, Nq, Nk, q_offsets, k_offsets, G, H, kv_heads, D,
+                                      scale, cap, bias, B, distance, distance_bytes, distance_offsets);
+  if (int rc = check_attention(a, float_type, Nq, Nk, G, H, kv_heads, D, B)) return rc;
+  if ((Nq > 0 && (q == nullptr || out == nullptr || lse == nullptr || dout == nullptr || dq == nullptr)) ||
+      (Nk > 0 && (k == nullptr || v == nullptr || dk == nullptr || dv == nullptr)))
+    return fail(TFG_ERR_INVALID_ARG, "NULL pointer");
+  if (dbias != nullptr && B == 0) return fail(TFG_ERR_INVALID_ARG, "dbias without a bias");
+  if (int wrc = check_ws(ws, ws_bytes, tfg_graph_attention_backward_ws_bytes(Nq, Nk, G, H, kv_heads, D, B)))
+    return wrc;
+  hipStream_t s = as_stream(stream);
+  int* err = static_cast<int*>(ws);
+  if (validate && G > 0)
+    if (int rc = launch_attention_check(a, err, s)) return rc;
+  if (int rc = launch_attention_backward(a, float_type, q, k, v, out, lse, dout, dq, dk, dv, dbias,
+                                         static_cast<char*>(ws) + 256, s))
+    return rc;
+  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder) : TFG_OK;
+}
+
+}  // extern "C"

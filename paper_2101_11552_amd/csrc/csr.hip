@@ -1357,4 +1357,45 @@ int build_graph(Graph& g, const void* src, const void* tgt, int index_type, void
   return TFG_OK;
 }
 
+// Ids sorted by value, stable: the sort of a graph's targets alone. key: the ids in
+// order; perm: where each came from; rowptr [V + 1]: the runs. col: n ints of scratch.
+// An id outside [0, V) counts as 0 and sets kErrIndex in `flag` (unless NULL).
+// Stream-ordered, nothing is read back.
+namespace {
+__global__ void flag_bad_tiles(const int* __restrict__ bad, int n, int* __restrict__ flag) {
+  int any = 0;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) any |= bad[i];
+  if (__syncthreads_or(any) && threadIdx.x == 0) *flag = kErrIndex;
+}
+}  // namespace
+
+size_t sort_ids_scratch_bytes(int64_t n, int64_t V) { return scratch_layout(n, V, 1).total; }
+
+int sort_ids(const void* ids, int index_type, int64_t n, int64_t V, int* key, int* perm, int* rowptr,
+             int* col, void* scratch, int* flag, hipStream_t s) {
+  Graph g;
+  g.E_in = g.E = n;
+  g.N = V;
+  g.N_src = 1;
+  g.rowptr = g.segptr = rowptr;
+  g.col = col;
+  g.perm = perm;
+  g.key = key;
+  const ScratchLayout L = scratch_layout(n, V, 1);
+  const SortPlan p = sort_plan(n, V, 1);
+  char* sc = static_cast<char*>(scratch);
+  int rc;
+#define TFG_SORT(I, T) sort_edges<I, T>(g, p, (const I*)nullptr, static_cast<const I*>(ids), sc, L, s)
+#define TFG_SORT_T(I) \
+  (p.threads == 256 ? TFG_SORT(I, 256) : p.threads == 512 ? TFG_SORT(I, 512) : TFG_SORT(I, 1024))
+  if (index_type == TFG_I64) rc = TFG_SORT_T(int64_t);
+  else rc = TFG_SORT_T(int32_t);
+#undef TFG_SORT_T
+#undef TFG_SORT
+  if (rc || flag == nullptr || n == 0) return rc;
+  flag_bad_tiles<<<1, 256, 0, s>>>(reinterpret_cast<const int*>(sc + L.bad), (int)p.ntiles, flag);
+  TFG_LAUNCHED("flag_bad_tiles");
+  return TFG_OK;
+}
+
 }  // namespace tfg

@@ -284,6 +284,8 @@ void launch_pool_grad(const float* dy, int64_t G, int F, const void* gi, int64_t
     pool_grad<IdxT, 1><<<nb, kBlock, 0, s>>>(dy, G, F, g, Nb, goff, reduce, arg, dx, ldx, lpr, lg, rows);
 }
 
+}  // namespace
+
 // The segment bounds (err NULL: nobody reads the flag).
 int launch_segment_bounds(const void* graph_index, int index_type, int64_t Nb, int64_t G,
                           int* goff, int* err, hipStream_t s) {
@@ -298,7 +300,11 @@ int launch_segment_bounds(const void* graph_index, int index_type, int64_t Nb, i
   return TFG_OK;
 }
 
-}  // namespace
+int launch_zero_flag(int* flag, hipStream_t s) {
+  zero_ints<<<1, 64, 0, s>>>(flag, 1);
+  TFG_LAUNCHED("zero_ints");
+  return TFG_OK;
+}
 
 int launch_segment_pool_backward(const float* dy, int64_t G, int64_t F, const void* graph_index,
                                  int index_type, int64_t Nb, int reduce, const int32_t* argmax,

@@ -172,6 +172,11 @@ int launch_segment_pool_backward(const float* dy, int64_t G, int64_t F, const vo
                                  int index_type, int64_t Nb, int reduce, const int32_t* argmax,
                                  float* dx, int64_t ldx, int* goff, int* err, hipStream_t s);
 
+// goff [G + 1]: first node of each graph of a sorted graph_index (any index: values in
+// [0, Nb]); bad ids set flags in err unless it is NULL.
+int launch_segment_bounds(const void* graph_index, int index_type, int64_t Nb, int64_t G,
+                          int* goff, int* err, hipStream_t s);
+int launch_zero_flag(int* flag, hipStream_t s);
 // softmax.hip: a_s = a_src . h and a_d = a_dst . h per (node, head)
 int launch_node_projections(const float* h, int64_t N, int H, int D, const float* a_src,
                             const float* a_dst, float* as, float* ad, hipStream_t s);
@@ -223,5 +228,60 @@ int launch_batch_graphs(int64_t G, const void* node_counts, const void* edge_cou
                         void* out_edge_index, void* out_graph_index, int* node_off, int* edge_off,
                         int* out_node_off, int* out_edge_off, int* sums, int* err,
                         hipStream_t s);
+
+// embed.hip
+struct Embed {
+  const void *table, *ids;
+  void* out;
+  int float_type, index_type;
+  int64_t V, F, ldt, N, pad;  // pad < 0: none
+  float scale;
+};
+int launch_embedding(const Embed& a, int* err, hipStream_t s);
+size_t embedding_backward_ws_bytes(int64_t N, int64_t V, int64_t F);
+// (table, ldt and out of `a` are not read; err: the first bytes of ws, or NULL)
+int launch_embedding_backward(const Embed& a, const void* dout, void* dtable, void* ws, int* err,
+                              hipStream_t s);
+// csr.hip: ids in [0, V) sorted by value (stable)
+size_t sort_ids_scratch_bytes(int64_t n, int64_t V);
+int sort_ids(const void* ids, int index_type, int64_t n, int64_t V, int* key, int* perm, int* rowptr,
+             int* col, void* scratch, int* flag, hipStream_t s);
+// group_norm.hip
+struct GroupNorm {
+  const void *x, *graph_index, *gamma, *beta, *dout;
+  void *out, *dx, *dgamma, *dbeta;
+  float *mean, *rstd;
+  int float_type, index_type, act;
+  int64_t Nb, F, ldx, G, K;
+  float eps;
+};
+size_t group_norm_ws_bytes(int64_t Nb, int64_t F, int64_t G, int64_t K, bool bwd);
+// The error flag inside the workspace.
+int* group_norm_flag(int64_t G, void* ws);
+int launch_group_norm(const GroupNorm& n, bool bwd, void* ws, int* err, hipStream_t s);
+
+// attention.hip, attention_grad.hip
+struct AttnShape {
+  const int *qoff, *koff;   // [G + 1] first query / key row of each graph
+  const int64_t* doff;      // [G] first distance byte of each graph, or NULL
+  const uint8_t* dist;
+  int64_t dist_bytes;
+  const void* bias;         // [H, B] of the features' type
+  int B;
+  int Nq, Nk, G, H, Hk, D;
+  float scale, cap;
+  int64_t ldq, ldk, ldv;
+};
+int max_attention_width();         // columns of a head
+int max_attention_bias_entries();  // (H / Hk) * B
+size_t attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk, int64_t D);
+int launch_attention(const AttnShape& a, int float_type, const void* q, const void* k,
+                     const void* v, void* out, float* lse, void* ws, hipStream_t s);
+size_t attention_backward_ws_bytes(int64_t Nq, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B);
+int launch_attention_backward(const AttnShape& a, int float_type, const void* q, const void* k,
+                              const void* v, const void* out, const float* lse, const void* dout,
+                              void* dq, void* dk, void* dv, void* dbias, void* ws, hipStream_t s);
+// Flags offsets outside [0, N], decreasing ones and distances outside their array in err.
+int launch_attention_check(const AttnShape& a, int* err, hipStream_t s);
 
 }  // namespace tfg
