@@ -629,8 +629,8 @@ int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int
  * exp(u). Rows outside every graph are left as they were.
  * Where there are few queries and many keys, the keys are split over blocks and
  * the parts joined in order.
- * Errors (validate): TFG_ERR_INDEX_RANGE for an offset outside [0, N] or distances
- * outside their array, TFG_ERR_UNSORTED for decreasing offsets.
+ * Errors (validate): TFG_ERR_UNSORTED for decreasing offsets, else TFG_ERR_INDEX_RANGE
+ * for an offset outside [0, N] or distances outside their array.
  *
  * Its gradient, from dout ([Nq, H*D]) and the forward's out and lse (all
  * contiguous): dq [Nq, H*D], dk, dv [Nk, kv_heads*D] (summed over the heads that

@@ -18,7 +18,8 @@ LIB = os.path.join(HERE, "libtfg.so")
 SOURCES = ["csr.hip", "norm.hip", "aggregate.hip", "slots_sum.hip", "slots_max.hip",
            "slots_heads.hip", "slots_masked.hip", "softmax.hip",
            "gat.hip", "gat_dot.hip", "pool.hip", "batch.hip", "backward.hip",
-           "embed.hip", "group_norm.hip", "attention.hip", "attention_grad.hip", "api.cpp"]
+           "embed.hip", "group_norm.hip", "attention.hip", "attention_bf16.hip", "attention_f32.hip", "attention_grad.hip",
+           "attention_grad_bf16.hip", "attention_grad_f32.hip", "api.cpp"]
 # measurement probes for the benchmark (include/tfg_probe.h), a library of their own
 PROBE_LIB = os.path.join(HERE, "libtfg_probe.so")
 PROBE_SOURCES = ["probe.hip"]

@@ -946,11 +946,14 @@ namespace {
 
 bool bad_float_type(int t) { return t != TFG_F32 && t != TFG_BF16; }
 
-// The device flag of a validated call, as a status.
-int read_flag(const int* err, hipStream_t s, const char* range, const char* order) {
+// The device flag of a validated call, as a status. order_first: ranges were judged by
+// the offsets, so that their order is reported before a range.
+int read_flag(const int* err, hipStream_t s, const char* range, const char* order,
+              bool order_first = false) {
   int flags = 0;
   const int* from[1] = {err};
   if (int rc = read_back(s, 1, from, &flags)) return rc;
+  if (order_first && (flags & kErrUnsorted)) return fail(TFG_ERR_UNSORTED, order);
   if (flags & kErrIndex) return fail(TFG_ERR_INDEX_RANGE, range);
   if (flags & kErrUnsorted) return fail(TFG_ERR_UNSORTED, order);
   return TFG_OK;
@@ -1183,7 +1186,7 @@ int tfg_graph_attention(const void *q, int64_t ldq, const void *k, int64_t ldk, 
     if (int rc = launch_attention_check(a, err, s)) return rc;
   if (int rc = launch_attention(a, float_type, q, k, v, out, lse, static_cast<char*>(ws) + 256, s))
     return rc;
-  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder) : TFG_OK;
+  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder, true) : TFG_OK;
 }
 
 size_t tfg_graph_attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H,
@@ -1217,7 +1220,7 @@ int tfg_graph_attention_backward(const void *dout, const void *q, int64_t ldq, c
   if (int rc = launch_attention_backward(a, float_type, q, k, v, out, lse, dout, dq, dk, dv, dbias,
                                          static_cast<char*>(ws) + 256, s))
     return rc;
-  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder) : TFG_OK;
+  return validate && G > 0 ? read_flag(err, s, kOffRange, kOffOrder, true) : TFG_OK;
 }
 
 }  // extern "C"

@@ -57,25 +57,49 @@ __device__ __forceinline__ unsigned load_buckets(const uint8_t* row, int j, int 
   return v;
 }
 
-// tanh: float32 features take the library's (its error is a few units of the last
-// place), bf16 ones 1 - 2 / (1 + exp(2 x)) on the hardware's exponential, whose
-// absolute error of some 2^-23 is far below the features' own rounding.
+// tanh. bf16 features: 1 - 2 / (1 + exp(2 x)) on the hardware's exponential and
+// reciprocal; its absolute error of some 2^-22 is far below the features' rounding.
+// float32 features: below 0.65 the odd polynomial x + x z P(z), z = x^2, P fitted to
+// (tanh(x) / x - 1) / z for the least relative error (8e-8 with its roundings), above it
+// the same form, whose error is a step or two there.
 template <typename T> __device__ __forceinline__ float cap_tanh(float x) {
   if constexpr (sizeof(T) == 4) {
-    return tanhf(x);
+    const float z = x * x;
+    float q = -0.005528633017092943f;
+    q = __builtin_fmaf(q, z, 0.020483314990997314f);
+    q = __builtin_fmaf(q, z, -0.05369296669960022f);
+    q = __builtin_fmaf(q, z, 0.1333089917898178f);
+    q = __builtin_fmaf(q, z, -0.3333326280117035f);
+    const float low = __builtin_fmaf(x * z, q, x);
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * kLog2e));
+    const float high = __builtin_copysignf(1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e), x);
+    return fabsf(x) < 0.65f ? low : high;  // (NaN: high, NaN)
   } else {
     const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
     return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e);
   }
 }
 
-// The bias of the group's heads, times log2(e), to LDS.
+// The biases of the group's heads to LDS, B + 1 a head: bucket B and above are
+// masked, -inf.
 template <typename T>
 __device__ __forceinline__ void load_bias(const AttnShape& a, int kvh, int grp, float* tab,
-                                          int threads) {
+                                          int threads, int tid) {
   const T* b = static_cast<const T*>(a.bias) + (int64_t)kvh * grp * a.B;
-  for (int i = threadIdx.x; i < grp * a.B; i += threads) tab[i] = (float)b[i] * kLog2e;
+  for (int i = tid; i < grp * (a.B + 1); i += threads) {
+    const int h = i / (a.B + 1), j = i - h * (a.B + 1);
+    tab[i] = j < a.B ? (float)b[h * a.B + j] : -INFINITY;
+  }
 }
+inline size_t bias_table_bytes(const AttnShape& a) {
+  return a.B > 0 ? sizeof(float) * (size_t)(a.H / a.Hk) * (a.B + 1) : 0;
+}
+
+// Capped scores are at most cap: up to this one their exponentials need no running
+// maximum (e^60 times 2^31 terms is far inside float32).
+constexpr float kBoundedCap = 60.0f;
+// Scores beyond this are differences of large numbers: see the kernels.
+constexpr float kHugeScore = 1.0e37f;
 
 // ROWS rows of D columns to LDS (row-major, leading dimension LD), zeros from
 // column D and row n on. at(r): a row's first element.

@@ -1,0 +1,387 @@
+// Attention inside each graph of a BatchGraph (gfx950), the forward kernels,
+// compiled per type in attention_bf16.hip and attention_f32.hip.
+//
+//   s = scale * <q, k>;  u = cap * tanh(s / cap) (cap > 0) + bias[head, dist];
+//   out = sum over the graph's unmasked keys of softmax(u) * v
+//
+// One pass over the keys with the running maximum m and sum l of the softmax:
+// a wavefront holds 16 * QT rows; for a tile of keys it forms S^T = K Q^T (a
+// row's scores in the four lanes l % 16 = row, in registers), rescales l and the
+// output by exp(m_old - m_new) where the maximum grew, and adds V^T P^T, whose
+// right operand is P^T as it lies in the registers (tiles.h). Keys pass through
+// LDS, row-major for the first product and as columns for the second; the next
+// tile's rows are on their way to registers meanwhile. Capped scores without a
+// bias are bounded by the cap, so that no maximum is kept for them.
+// Scores, maximum, sum and output are float32; P is rounded to the features'
+// type for its product (bf16: half a step, 2^-9 of each weight at most, as the
+// output's own rounding).
+#pragma once
+
+#include "attention.h"
+
+namespace tfg {
+
+struct AttnFwd {
+  AttnShape a;
+  const void *q, *k, *v;
+  void* out;
+  float* lse;
+  int vec_q, vec_k, vec_v, vec_o;
+  int nsplit;      // > 1: the keys of a graph in that many parts, joined afterwards
+  float* part;     // [nsplit][Nq * H][D] unnormalised partial outputs
+  float* part_ml;  // [nsplit][Nq * H][2] their maximum and sum
+  int small;       // graphs of at most so many queries and keys are another launch's
+  int heads;       // key/value heads a block takes
+};
+
+template <typename T, int DP, int WAVES, int QT, bool BIAS, bool CAP>
+__global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
+  constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDV = BN + lds_pad<T>();
+  constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
+  // staging units of a thread: rows of eight columns (K), four rows of eight (V)
+  constexpr int KU = (BN * DP / 8 + THREADS - 1) / THREADS;
+  constexpr int VU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
+  // the next tile waits in registers where it takes at most 48 of them
+  constexpr bool AHEAD = (KU * 8 + VU * 32) * sizeof(T) / 4 <= 48;
+  __shared__ T Ks[BN * LDK];
+  __shared__ T Vt[DP * LDV];
+  extern __shared__ float tab[];
+  const AttnShape& a = p.a;
+  const int grp = a.H / a.Hk, D = a.D;
+  const int per_slot = (a.Hk + p.heads - 1) / p.heads;
+  const int64_t slot = blockIdx.x / per_slot;
+  const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
+  const Span s = find_span<BM>(a, a.qoff, a.Nq, grp, slot);
+  const int64_t M = (int64_t)s.nq * grp;
+  const int64_t r0 = (int64_t)s.tile * BM;
+  if (s.g < 0 || r0 >= M || (s.nq <= p.small && s.nk <= p.small)) return;
+  const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+  const int wave = uniform((int)threadIdx.x / kWave);
+  const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
+  const int tiles = (s.nk + BN - 1) / BN;
+  const int per = (tiles + p.nsplit - 1) / p.nsplit;
+  const int t0 = min((int)blockIdx.y * per, tiles), t1 = min(t0 + per, tiles);
+  const bool flip = a.scale < 0.0f;  // the maximum is taken over raw products: q changes sign
+  const float scale = fabsf(a.scale), scale2 = scale * kLog2e;
+  const float to_tanh = CAP ? scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
+  const bool bounded = CAP && !BIAS && a.cap <= kBoundedCap;
+
+  // this lane's rows (one a query tile)
+  int qi[QT], hg[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int64_t r = r0 + (wave * QT + t) * 16 + col;
+    qi[t] = r < M ? (int)(r / grp) : -1;
+    hg[t] = r < M ? (int)(r - (int64_t)qi[t] * grp) : 0;
+  }
+  const bool idle = r0 + wave * (QT * 16) >= M;  // a wavefront without rows only stages
+
+  for (int kvh = kvh0; kvh < min(kvh0 + p.heads, a.Hk); ++kvh) {
+    if (BIAS) {
+      __syncthreads();
+      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+    }
+    frag_t<T, DP> qf[QT][KC];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const T* row = static_cast<const T*>(p.q) + (int64_t)(s.q0 + max(qi[t], 0)) * a.ldq +
+                     (int64_t)(kvh * grp + hg[t]) * D;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        qf[t][c] = zero_frag<T, DP>();
+        if (qi[t] >= 0) qf[t][c] = load_frag<T, DP>(row, c, g, D, p.vec_q);
+        if (flip) qf[t][c] = -qf[t][c];
+      }
+    }
+    float m[QT], l[QT];
+    f32x4 o[QT][DT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      m[t] = bounded ? 0.0f : -INFINITY;
+      l[t] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    x8_t<T> kr[KU], vr[VU][4];
+    unsigned bk[QT][KT];
+    const auto fetch = [&](int kt) {  // the rows of tile kt to registers
+      const int j0 = kt * BN, n = min(BN, s.nk - j0);
+      const T* kp = static_cast<const T*>(p.k) + (int64_t)(s.k0 + j0) * a.ldk + (int64_t)kvh * D;
+      const T* vp = static_cast<const T*>(p.v) + (int64_t)(s.k0 + j0) * a.ldv + (int64_t)kvh * D;
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) kr[u][e] = (T)0.0f;
+        if (r < n) kr[u] = load8<T>(kp + r * a.ldk, d0, D, p.vec_k);
+      }
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) vr[u][i][e] = (T)0.0f;
+          if (quad * 4 + i < n && d0 < DP)
+            vr[u][i] = load8<T>(vp + (quad * 4 + i) * a.ldv, d0, D, p.vec_v);
+        }
+      }
+    };
+    const auto fetch_buckets = [&](int kt) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const uint8_t* row = dist + (int64_t)max(qi[t], 0) * s.nk;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+          bk[t][x] = dist == nullptr ? 0xFFFFFFFFu : load_buckets(row, kt * BN + x * 16 + g * 4, s.nk);
+      }
+    };
+    if (t0 < t1) {
+      if (AHEAD) fetch(t0);
+      if (BIAS) fetch_buckets(t0);
+    }
+    for (int kt = t0; kt < t1; ++kt) {
+      const int n = min(BN, s.nk - kt * BN);
+      if (!AHEAD) fetch(kt);
+      __syncthreads();  // the last tile has been used
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
+        if (r < BN) put8<T>(Ks + r * LDK + d0, kr[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
+        if (d0 < DP) {
+          const int place = interleaved_quad(quad);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x4_t<T> w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = vr[u][i][e];
+            *reinterpret_cast<x4_t<T>*>(Vt + (d0 + e) * LDV + place) = w;
+          }
+        }
+      }
+      __syncthreads();
+      if (AHEAD && kt + 1 < t1) fetch(kt + 1);
+      if (idle) continue;
+      f32x4 sc[QT][KT];
+#pragma unroll
+      for (int x = 0; x < KT; ++x) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sc[t][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const frag_t<T, DP> kf = lds_frag<T, DP>(Ks + (x * 16 + col) * LDK, c, g);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) sc[t][x] = mma(kf, qf[t][c], sc[t][x]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        // scores: natural units with a bias, raw products without one, base 2 where bounded
+        if constexpr (BIAS) {
+          const float* th = tab + hg[t] * (a.B + 1);
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned b = min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B);
+              const float add = th[b];
+              // (a select: whatever a masked pair's product is, NaN too, it is masked)
+              const float u = CAP ? __builtin_fmaf(a.cap, cap_tanh<T>(sc[t][x][i] * to_tanh), add)
+                                  : __builtin_fmaf(sc[t][x][i], scale, add);
+              sc[t][x][i] = b == (unsigned)a.B || add == -INFINITY ? -INFINITY : u;
+            }
+        } else {
+          if constexpr (CAP) {
+            const float f = bounded ? cap2 : a.cap;
+#pragma unroll
+            for (int x = 0; x < KT; ++x)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) sc[t][x][i] = f * cap_tanh<T>(sc[t][x][i] * to_tanh);
+          }
+          if (n < BN) {
+#pragma unroll
+            for (int x = 0; x < KT; ++x)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (x * 16 + g * 4 + i >= n) sc[t][x][i] = -INFINITY;
+          }
+        }
+        float sum = 0.0f;
+        if (bounded) {
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sc[t][x][i] = __builtin_amdgcn_exp2f(sc[t][x][i]);
+              sum += sc[t][x][i];
+            }
+          l[t] += sum;
+          continue;
+        }
+        const float unit = BIAS || CAP ? kLog2e : scale2;  // one unit of a score in base 2
+        float mx = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+          mx = fmaxf(fmaxf(fmaxf(mx, sc[t][x][0]), fmaxf(sc[t][x][1], sc[t][x][2])), sc[t][x][3]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = fmaxf(m[t], mx);
+        float base = mn == -INFINITY ? 0.0f : mn;  // (nothing unmasked so far)
+        if (__ballot(mn > m[t]) != 0) {
+          const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * unit);
+          l[t] *= alpha;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+          m[t] = mn;
+        }
+        if (BIAS && __ballot(fabsf(base) > kHugeScore) != 0) {
+          // a bias of the type's lowest value: base * log2(e) would overflow
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[t][x][i] -= base;
+          base = 0.0f;
+        }
+        const float off = -base * unit;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sc[t][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][i], unit, off));
+            sum += sc[t][x][i];
+          }
+        l[t] += sum;
+      }
+      if (BIAS && kt + 1 < t1) fetch_buckets(kt + 1);
+#pragma unroll
+      for (int x = 0; x < KT / 2; ++x) {
+        x8_t<T> pf[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) pf[t] = as_operand<T>(sc[t][2 * x], sc[t][2 * x + 1]);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const x8_t<T> vf = lds8<T>(Vt + (d * 16 + col) * LDV + x * 32 + g * 8);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][d] = mma(vf, pf[t], o[t][d]);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      l[t] += __shfl_xor(l[t], 16);
+      l[t] += __shfl_xor(l[t], 32);
+      if (qi[t] < 0) continue;
+      const int64_t row = (int64_t)(s.q0 + qi[t]) * a.H + kvh * grp + hg[t];
+      // the maximum in natural units
+      const float mu = BIAS || CAP || m[t] == -INFINITY ? m[t] : m[t] * scale;
+      if (p.nsplit > 1) {
+        const int64_t at = (int64_t)blockIdx.y * a.Nq * a.H + row;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          store4<float>(p.part + at * D, d * 16 + g * 4, D, D % 4 == 0 ? 4 : 1, o[t][d]);
+        if (g == 0) {
+          p.part_ml[2 * at] = mu;
+          p.part_ml[2 * at + 1] = l[t];
+        }
+        continue;
+      }
+      // a row without unmasked keys: zeros, and -inf as its log-sum
+      const float inv = l[t] == 0.0f ? 0.0f : 1.0f / l[t];
+      T* orow = static_cast<T*>(p.out) + row * D;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) store4<T>(orow, d * 16 + g * 4, D, p.vec_o, o[t][d] * inv);
+      if (p.lse != nullptr && g == 0)
+        p.lse[row] = l[t] == 0.0f ? -INFINITY : mu + log2f(l[t]) * kLn2;
+    }
+  }
+}
+
+// Joins the parts of each (query, head): one wavefront a row, lanes over the
+// columns. Rows outside every graph are left as they were.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void attn_join(AttnFwd p) {
+  const AttnShape& a = p.a;
+  const int64_t rows = (int64_t)a.Nq * a.H;
+  const int64_t row = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
+  const int q = (int)(row / a.H);
+  if (row >= rows || q < a.qoff[0] || q >= a.qoff[a.G]) return;
+  const int lane = lane_id();
+  float m = -INFINITY;
+  for (int sp = 0; sp < p.nsplit; ++sp)
+    if (p.part_ml[2 * (sp * rows + row) + 1] != 0.0f) m = fmaxf(m, p.part_ml[2 * (sp * rows + row)]);
+  const float base = m == -INFINITY ? 0.0f : m;
+  float l = 0.0f, acc[kMaxHeadDim / kWave] = {};
+  for (int sp = 0; sp < p.nsplit; ++sp) {
+    const float lp = p.part_ml[2 * (sp * rows + row) + 1];
+    if (lp == 0.0f) continue;  // (no keys in this part, or none unmasked)
+    const float w = __builtin_amdgcn_exp2f((p.part_ml[2 * (sp * rows + row)] - base) * kLog2e);
+    l += w * lp;
+#pragma unroll
+    for (int c = 0; c < kMaxHeadDim / kWave; ++c)
+      if (c * kWave + lane < a.D) acc[c] += w * p.part[(sp * rows + row) * a.D + c * kWave + lane];
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+  for (int c = 0; c < kMaxHeadDim / kWave; ++c)
+    if (c * kWave + lane < a.D)
+      static_cast<T*>(p.out)[row * a.D + c * kWave + lane] = to_type<T>(acc[c] * inv);
+  if (p.lse != nullptr && lane == 0) p.lse[row] = l == 0.0f ? -INFINITY : m + log2f(l) * kLn2;
+}
+
+template <typename T, int DP, int WAVES, int QT>
+int launch_fwd(AttnFwd& p, hipStream_t s) {
+  constexpr int BM = WAVES * QT * 16;
+  const int grp = p.a.H / p.a.Hk;
+  const int64_t slots = (int64_t)p.a.Nq * grp / BM + p.a.G;
+  const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
+  if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
+  const dim3 grid((unsigned)blocks, (unsigned)p.nsplit);
+  const size_t lds = bias_table_bytes(p.a);
+  const bool cap = p.a.cap > 0.0f;
+  if (p.a.B > 0) {
+    if (cap) attn_fwd<T, DP, WAVES, QT, true, true><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, true, false><<<grid, WAVES * kWave, lds, s>>>(p);
+  } else {
+    if (cap) attn_fwd<T, DP, WAVES, QT, false, true><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, false, false><<<grid, WAVES * kWave, lds, s>>>(p);
+  }
+  TFG_LAUNCHED("attn_fwd");
+  if (p.nsplit > 1) {
+    const int64_t rows = (int64_t)p.a.Nq * p.a.H;
+    attn_join<T><<<(unsigned)((rows + 3) / 4), kBlock, 0, s>>>(p);
+    TFG_LAUNCHED("attn_join");
+  }
+  return TFG_OK;
+}
+
+template <typename T, int DP>
+int launch_fwd_rows(AttnFwd& p, hipStream_t s) {
+  const int64_t rows = (int64_t)p.a.Nq * (p.a.H / p.a.Hk) / std::max(p.a.G, 1);
+  if (rows <= 16) return launch_fwd<T, DP, 1, 1>(p, s);
+  if (rows <= 192) return launch_fwd<T, DP, 4, 1>(p, s);
+  return launch_fwd<T, DP, 4, 2>(p, s);
+}
+
+template <typename T>
+int launch_fwd_type(AttnFwd& p, hipStream_t s) {
+  const int D = p.a.D;
+  p.vec_q = row_vector<T>(p.q, p.a.ldq, D);
+  p.vec_k = row_vector<T>(p.k, p.a.ldk, D);
+  p.vec_v = row_vector<T>(p.v, p.a.ldv, D);
+  p.vec_o = row_vector<T>(p.out, (int64_t)p.a.H * D, D);
+  p.heads = 1;
+  if (D <= 16) return launch_fwd_rows<T, 16>(p, s);
+  if (D <= 32) return launch_fwd_rows<T, 32>(p, s);
+  if (D <= 64) return launch_fwd_rows<T, 64>(p, s);
+  return launch_fwd_rows<T, 128>(p, s);
+}
+
+int launch_fwd_bf16(AttnFwd& p, hipStream_t s);
+int launch_fwd_f32(AttnFwd& p, hipStream_t s);
+
+}  // namespace tfg

@@ -1,0 +1,706 @@
+// Gradients of the attention inside each graph of a BatchGraph (gfx950), the
+// kernels, compiled per type in attention_grad_bf16.hip and attention_grad_f32.hip.
+//
+// With p = exp(u - lse) formed again from the forward's log-sum and
+// delta[row] = <dout[row], out[row]> (= the sum of p dp over the keys):
+//   dv = p^T dout;  dp = dout v^T;  du = p (dp - delta);
+//   dbias[head, b] = sum of du over the pairs of bucket b;
+//   ds = du (1 - tanh^2) (capped scores);  dq = scale ds k;  dk = scale ds^T q
+// Two passes, each of which owns its outputs (no float atomics between lanes, a
+// fixed order of every sum): attn_grad_q over tiles of rows (delta, dq and the
+// bias), then attn_grad_kv over tiles of keys (dk, dv), over the queries of all
+// heads that share the key/value head. Scores and dp are formed in both: seven
+// products instead of five, and no partial dq in memory.
+//
+// delta from a bf16 output carries that output's rounding, which short rows feel
+// (a node's weights are large there): up to two tiles of keys it is summed from p
+// and dp in a first sweep instead. The same sweep serves rows whose log-sum is so
+// large (a bias of the type's lowest value) that u - lse has lost the sum: it keeps
+// the maximum and the sum apart.
+#pragma once
+
+#include "attention.h"
+#include "columns.h"
+
+namespace tfg {
+
+struct AttnGrad {
+  AttnShape a;
+  const void *q, *k, *v, *out, *dout;
+  const float* lse;
+  void *dq, *dk, *dv;
+  // per (query, head): p = exp2((u - row_a) * log2(e) + row_c) with a bias, else
+  // exp2(u in base 2 - row_a); +inf: a row without unmasked keys
+  float *row_a, *row_c, *row_delta;
+  float* bias_part;  // [slots][H * B] partial bias gradients, or NULL
+  int vec_q, vec_k, vec_v, vec_o, vec_do, vec_dq, vec_dk, vec_dv;
+  int copies;        // bias bins a wavefront keeps: one, or one a query tile
+  int small;         // graphs of at most so many queries and keys are another launch's
+  int heads;         // key/value heads a block takes
+};
+
+// Beyond this log-sum its rounding (2^-24 of it) is felt in exp(u - lse).
+constexpr float kLongLse = 4096.0f;
+
+struct ScoreScale {
+  float scale, to_tanh, unit, cap;  // unit: from what score() gives to base 2
+};
+template <bool BIAS, bool CAP>
+__device__ __forceinline__ ScoreScale score_scale(const AttnShape& a) {
+  return ScoreScale{a.scale, CAP ? a.scale / a.cap : 0.0f,
+                    BIAS ? kLog2e : CAP ? a.cap * kLog2e : a.scale * kLog2e, a.cap};
+}
+// A raw product as a score (natural units with a bias, else times unit in base 2)
+// and the cap's derivative there. add: -inf masks, whatever the product is.
+template <typename T, bool BIAS, bool CAP>
+__device__ __forceinline__ float score(float x, float add, const ScoreScale& c, float* slope) {
+  float u = x;
+  if constexpr (CAP) {
+    const float t = cap_tanh<T>(x * c.to_tanh);
+    *slope = __builtin_fmaf(-t, t, 1.0f);
+    u = t;
+  } else {
+    *slope = 1.0f;
+  }
+  if constexpr (BIAS) {
+    u = __builtin_fmaf(u, CAP ? c.cap : c.scale, add);
+    return add == -INFINITY ? -INFINITY : u;
+  }
+  return u;
+}
+template <bool BIAS>
+__device__ __forceinline__ float weight(float u, float unit, float ra, float rc) {
+  if constexpr (BIAS) return __builtin_amdgcn_exp2f(__builtin_fmaf(u - ra, unit, rc));
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(u, unit, -ra));
+}
+
+template <typename T, int DP, int WAVES, int QT, bool BIAS, bool CAP>
+__global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
+  constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
+  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BN + lds_pad<T>();
+  constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
+  // staging units of a thread: four rows of eight columns (K), rows of eight (V)
+  constexpr int KU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
+  constexpr int VU = (BN * (DP / 8) + THREADS - 1) / THREADS;
+  constexpr bool AHEAD = (KU * 32 + VU * 8) * sizeof(T) / 4 <= 48;
+  __shared__ T Ks[BN * LDK];
+  __shared__ T Vs[BN * LDK];
+  __shared__ T Kt[DP * LDT];
+  extern __shared__ float tab[];
+  const AttnShape& a = p.a;
+  const int grp = a.H / a.Hk, D = a.D;
+  const int per_slot = (a.Hk + p.heads - 1) / p.heads;
+  const int64_t slot = blockIdx.x / per_slot;
+  const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
+  const int kvh1 = min(kvh0 + p.heads, a.Hk);
+  const bool want_bias = BIAS && p.bias_part != nullptr;
+  float* bins = tab + grp * (a.B + 1);  // [WAVES][copies][B + 1][64], one column a lane
+  const Span s = find_span<BM>(a, a.qoff, a.Nq, grp, slot);
+  const int64_t M = (int64_t)s.nq * grp;
+  const int64_t r0 = (int64_t)s.tile * BM;
+  if (s.g < 0 || r0 >= M || (s.nq <= p.small && s.nk <= p.small)) {
+    if (want_bias)
+      for (int i = threadIdx.x; i < (kvh1 - kvh0) * grp * a.B; i += THREADS)
+        p.bias_part[(slot * a.H + (int64_t)kvh0 * grp) * a.B + i] = 0.0f;
+    return;
+  }
+  const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+  const int wave = uniform((int)threadIdx.x / kWave);
+  const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
+  const int tiles = (s.nk + BN - 1) / BN;
+  const ScoreScale sx = score_scale<BIAS, CAP>(a);
+  int qi[QT], hg[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int64_t r = r0 + (wave * QT + t) * 16 + col;
+    qi[t] = r < M ? (int)(r / grp) : -1;
+    hg[t] = r < M ? (int)(r - (int64_t)qi[t] * grp) : 0;
+  }
+  const bool idle = r0 + wave * (QT * 16) >= M;  // a wavefront without rows only stages
+
+  for (int kvh = kvh0; kvh < kvh1; ++kvh) {
+    if (BIAS) {
+      __syncthreads();
+      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+      if (want_bias)
+        for (int i = threadIdx.x; i < WAVES * p.copies * (a.B + 1) * kWave; i += THREADS) bins[i] = 0.0f;
+    }
+    float ra[QT], rc[QT], delta[QT];
+    frag_t<T, DP> qf[QT][KC], df[QT][KC];
+    bool again = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int64_t node = s.q0 + max(qi[t], 0);
+      const int head = kvh * grp + hg[t];
+      const T* qrow = static_cast<const T*>(p.q) + node * a.ldq + (int64_t)head * D;
+      const int64_t at = (node * a.H + head) * D;
+      float dsum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        qf[t][c] = df[t][c] = zero_frag<T, DP>();
+        if (qi[t] >= 0) {
+          qf[t][c] = load_frag<T, DP>(qrow, c, g, D, p.vec_q);
+          df[t][c] = load_frag<T, DP>(static_cast<const T*>(p.dout) + at, c, g, D, p.vec_do);
+          const frag_t<T, DP> of = load_frag<T, DP>(static_cast<const T*>(p.out) + at, c, g, D, p.vec_o);
+#pragma unroll
+          for (int e = 0; e < Frag<T, DP>::N; ++e) dsum += (float)df[t][c][e] * (float)of[e];
+        }
+      }
+      dsum += __shfl_xor(dsum, 16);
+      dsum += __shfl_xor(dsum, 32);
+      delta[t] = dsum;
+      ra[t] = INFINITY;  // p = 0
+      rc[t] = 0.0f;
+      if (qi[t] >= 0) {
+        const float ls = p.lse[node * a.H + head];
+        if (ls != -INFINITY) ra[t] = BIAS ? ls : ls * kLog2e;
+        again = again || (BIAS && ls != -INFINITY && fabsf(ls) > kLongLse);
+      }
+    }
+    again = (sizeof(T) == 2 && tiles <= 2) || (BIAS && __syncthreads_or(again));
+
+    x8_t<T> kr[KU][4], vr[VU];
+    unsigned bk[QT][KT];
+    const auto fetch = [&](int kt) {
+      const int j0 = kt * BN, n = min(BN, s.nk - j0);
+      const T* kp = static_cast<const T*>(p.k) + (int64_t)(s.k0 + j0) * a.ldk + (int64_t)kvh * D;
+      const T* vp = static_cast<const T*>(p.v) + (int64_t)(s.k0 + j0) * a.ldv + (int64_t)kvh * D;
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) kr[u][i][e] = (T)0.0f;
+          if (quad * 4 + i < n && d0 < DP)
+            kr[u][i] = load8<T>(kp + (quad * 4 + i) * a.ldk, d0, D, p.vec_k);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vr[u][e] = (T)0.0f;
+        if (r < n) vr[u] = load8<T>(vp + r * a.ldv, d0, D, p.vec_v);
+      }
+    };
+    const auto place_tile = [&]() {  // the fetched rows to LDS
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
+        if (d0 < DP) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) put8<T>(Ks + (quad * 4 + i) * LDK + d0, kr[u][i]);
+          const int place = interleaved_quad(quad);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x4_t<T> w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = kr[u][i][e];
+            *reinterpret_cast<x4_t<T>*>(Kt + (d0 + e) * LDT + place) = w;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
+        if (r < BN) put8<T>(Vs + r * LDK + d0, vr[u]);
+      }
+    };
+    const auto fetch_buckets = [&](int kt) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const uint8_t* row = dist + (int64_t)max(qi[t], 0) * s.nk;
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+          bk[t][x] = dist == nullptr ? 0xFFFFFFFFu : load_buckets(row, kt * BN + x * 16 + g * 4, s.nk);
+      }
+    };
+    // raw products and dp of key tile x
+    const auto products = [&](int x, f32x4 (&sc)[QT], f32x4 (&dp)[QT]) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t) sc[t] = dp[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const frag_t<T, DP> kf = lds_frag<T, DP>(Ks + (x * 16 + col) * LDK, c, g);
+        const frag_t<T, DP> vf = lds_frag<T, DP>(Vs + (x * 16 + col) * LDK, c, g);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          sc[t] = mma(kf, qf[t][c], sc[t]);
+          dp[t] = mma(vf, df[t][c], dp[t]);
+        }
+      }
+    };
+
+    if (again) {
+      // first sweep: maximum, sum of exp and sum of exp * dp of every row
+      float m[QT], l[QT], w[QT];
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = w[t] = 0.0f;
+      }
+      for (int kt = 0; kt < tiles; ++kt) {
+        const int n = min(BN, s.nk - kt * BN);
+        fetch(kt);
+        if (BIAS) fetch_buckets(kt);
+        __syncthreads();
+        place_tile();
+        __syncthreads();
+        if (idle) continue;
+        for (int x = 0; x < KT && x * 16 < n; ++x) {
+          f32x4 sc[QT], dp[QT];
+          products(x, sc, dp);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) {
+            unsigned b4 = bk[t][0];
+#pragma unroll
+            for (int y = 1; y < KT; ++y) b4 = x == y ? bk[t][y] : b4;
+            float mx = m[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned b = min((b4 >> (8 * i)) & 0xFFu, (unsigned)a.B);
+              float slope;
+              float u = score<T, BIAS, CAP>(sc[t][i], BIAS ? tab[hg[t] * (a.B + 1) + b] : 0.0f, sx, &slope);
+              if (!BIAS) u = x * 16 + g * 4 + i < n ? u * sx.unit : -INFINITY;
+              sc[t][i] = u;
+              mx = fmaxf(mx, u);
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float base = mx == -INFINITY ? 0.0f : mx;
+            const float unit = BIAS ? kLog2e : 1.0f;
+            const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * unit);
+            l[t] *= alpha;
+            w[t] *= alpha;
+            m[t] = mx;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float e = __builtin_amdgcn_exp2f((sc[t][i] - base) * unit);
+              l[t] += e;
+              if (sc[t][i] != -INFINITY) w[t] += e * dp[t][i];
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        l[t] += __shfl_xor(l[t], 16);
+        l[t] += __shfl_xor(l[t], 32);
+        w[t] += __shfl_xor(w[t], 16);
+        w[t] += __shfl_xor(w[t], 32);
+        if (l[t] == 0.0f) continue;  // (no rows, or none unmasked: p = 0 already)
+        delta[t] = w[t] / l[t];
+        if (BIAS) {
+          ra[t] = m[t];
+          rc[t] = -log2f(l[t]);
+        } else {
+          ra[t] = m[t] + log2f(l[t]);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+      if (qi[t] >= 0 && g == 0) {
+        const int64_t at = (int64_t)(s.q0 + qi[t]) * a.H + kvh * grp + hg[t];
+        p.row_a[at] = ra[t];
+        if (BIAS) p.row_c[at] = rc[t];
+        p.row_delta[at] = delta[t];
+      }
+
+    f32x4 o[QT][DT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (tiles > 0) {
+      if (AHEAD) fetch(0);
+      if (BIAS) fetch_buckets(0);
+    }
+    for (int kt = 0; kt < tiles; ++kt) {
+      const int n = min(BN, s.nk - kt * BN);
+      if (!AHEAD) fetch(kt);
+      __syncthreads();
+      place_tile();
+      __syncthreads();
+      if (AHEAD && kt + 1 < tiles) fetch(kt + 1);
+      if (idle) continue;
+#pragma unroll
+      for (int x2 = 0; x2 < KT / 2; ++x2) {
+        if (x2 * 32 >= n) break;
+        f32x4 sc[2][QT], dp[2][QT];
+        products(2 * x2, sc[0], dp[0]);
+        products(2 * x2 + 1, sc[1], dp[1]);
+        x8_t<T> sf[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          const float* th = tab + hg[t] * (a.B + 1);
+          float* bin = bins + (wave * p.copies + (p.copies > 1 ? t : 0)) * (a.B + 1) * kWave + lane;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int x = 2 * x2 + h;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned b = BIAS ? min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
+              const float add = BIAS ? th[b] : 0.0f;
+              float slope;
+              const float u = score<T, BIAS, CAP>(sc[h][t][i], add, sx, &slope);
+              const bool live = BIAS ? add != -INFINITY : x * 16 + g * 4 + i < n;
+              float du = weight<BIAS>(u, sx.unit, ra[t], rc[t]) * (dp[h][t][i] - delta[t]);
+              du = live ? du : 0.0f;
+              // (one lane adds to a bin: the order of its additions is the program's)
+              if (want_bias)
+                __hip_atomic_fetch_add(bin + b * kWave, du, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+              sc[h][t][i] = du * slope;
+            }
+          }
+          sf[t] = as_operand<T>(sc[0][t], sc[1][t]);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const x8_t<T> kf = lds8<T>(Kt + (d * 16 + col) * LDT + x2 * 32 + g * 8);
+#pragma unroll
+          for (int t = 0; t < QT; ++t) o[t][d] = mma(kf, sf[t], o[t][d]);
+        }
+      }
+      if (BIAS && kt + 1 < tiles) fetch_buckets(kt + 1);
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      if (qi[t] < 0) continue;
+      T* row = static_cast<T*>(p.dq) + ((int64_t)(s.q0 + qi[t]) * a.H + kvh * grp + hg[t]) * D;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) store4<T>(row, d * 16 + g * 4, D, p.vec_dq, o[t][d] * a.scale);
+    }
+    if (!want_bias) continue;
+    __syncthreads();
+    // (head, bucket) sums of the bins; neighbouring buckets start at other lanes, so
+    // that they read other banks
+    for (int i = threadIdx.x; i < grp * a.B; i += THREADS) {
+      const int h = i / a.B, b = i % a.B;
+      float sum = 0.0f;
+      for (int w = 0; w < WAVES * p.copies; ++w) {
+        // the row of column c in this bin is (w * 16 + c) past the tile's first, up to
+        // a multiple of the group where one bin serves every query tile
+        const int first = p.copies > 1 || QT == 1 ? w * 16 : 0;
+        const int base = (int)((r0 + first) % grp);
+        for (int e = 0; e < kWave; ++e) {
+          const int ln = (e + b) & (kWave - 1);
+          if ((base + (ln & 15)) % grp == h) sum += bins[(w * (a.B + 1) + b) * kWave + ln];
+        }
+      }
+      p.bias_part[(slot * a.H + (int64_t)kvh * grp) * a.B + i] = sum;
+    }
+  }
+}
+
+// Byte j of four neighbouring lanes' words, for lane j of them: from the rows of a
+// 4 x 4 block of buckets, one a lane, to its columns.
+__device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
+  const unsigned r0 = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x00, 0xF, 0xF, true);
+  const unsigned r1 = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x55, 0xF, 0xF, true);
+  const unsigned r2 = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xAA, 0xF, 0xF, true);
+  const unsigned r3 = (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xFF, 0xF, 0xF, true);
+  const unsigned sel = j | ((4 + j) << 8);
+  const unsigned lo = __builtin_amdgcn_perm(r1, r0, sel), hi = __builtin_amdgcn_perm(r3, r2, sel);
+  return (lo & 0xFFFFu) | (hi << 16);
+}
+
+template <typename T, int DP, int WAVES, int KT, bool BIAS, bool CAP>
+__global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
+  constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
+  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BR + lds_pad<T>();
+  constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, XT = BR / 16;
+  constexpr int RU = (BR / 4 * (DP / 8) + THREADS - 1) / THREADS;  // four rows of eight columns
+  constexpr bool AHEAD = RU * 64 * sizeof(T) / 4 <= 64;
+  __shared__ T Qs[BR * LDK];
+  __shared__ T Os[BR * LDK];
+  __shared__ T Qt[DP * LDT];
+  __shared__ T Ot[DP * LDT];
+  __shared__ float rows[3][BR];  // row_a, row_c, delta
+  extern __shared__ float tab[];
+  const AttnShape& a = p.a;
+  const int grp = a.H / a.Hk, D = a.D;
+  const int per_slot = (a.Hk + p.heads - 1) / p.heads;
+  const int64_t slot = blockIdx.x / per_slot;
+  const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
+  const Span s = find_span<BK>(a, a.koff, a.Nk, 1, slot);
+  const int64_t kt0 = (int64_t)s.tile * BK;
+  if (s.g < 0 || kt0 >= s.nk || (s.nq <= p.small && s.nk <= p.small)) return;
+  const int lane = lane_id(), col = lane & 15, g = lane >> 4;
+  const int wave = uniform((int)threadIdx.x / kWave);
+  const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
+  const ScoreScale sx = score_scale<BIAS, CAP>(a);
+  const bool idle = kt0 + wave * (KT * 16) >= s.nk;  // a wavefront without keys only stages
+  int key[KT];
+#pragma unroll
+  for (int t = 0; t < KT; ++t) {
+    const int64_t j = kt0 + (wave * KT + t) * 16 + col;
+    key[t] = j < s.nk ? (int)j : -1;
+  }
+  const int rtiles = (s.nq + BR - 1) / BR;
+
+  for (int kvh = kvh0; kvh < min(kvh0 + p.heads, a.Hk); ++kvh) {
+    if (BIAS) {
+      __syncthreads();
+      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+    }
+    frag_t<T, DP> kf[KT][KC], vf[KT][KC];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const int64_t node = s.k0 + max(key[t], 0);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        kf[t][c] = vf[t][c] = zero_frag<T, DP>();
+        if (key[t] >= 0) {
+          kf[t][c] = load_frag<T, DP>(static_cast<const T*>(p.k) + node * a.ldk + (int64_t)kvh * D, c, g, D, p.vec_k);
+          vf[t][c] = load_frag<T, DP>(static_cast<const T*>(p.v) + node * a.ldv + (int64_t)kvh * D, c, g, D, p.vec_v);
+        }
+      }
+    }
+    f32x4 dk[KT][DT], dv[KT][DT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) dk[t][d] = dv[t][d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    x8_t<T> qr[RU][4], dr[RU][4];
+    float rv[3];
+    unsigned bk[KT][XT];
+    // tile i of the group's heads, one after the other
+    const auto fetch = [&](int i) {
+      const int head = kvh * grp + i / rtiles, q0 = (i % rtiles) * BR, n = min(BR, s.nq - q0);
+      const T* qp = static_cast<const T*>(p.q) + (int64_t)(s.q0 + q0) * a.ldq + (int64_t)head * D;
+      const int64_t ldo = (int64_t)a.H * D;
+      const T* dp = static_cast<const T*>(p.dout) + (int64_t)(s.q0 + q0) * ldo + (int64_t)head * D;
+#pragma unroll
+      for (int u = 0; u < RU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BR / 4), d0 = (c / (BR / 4)) * 8;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) qr[u][e4][e] = dr[u][e4][e] = (T)0.0f;
+          if (quad * 4 + e4 < n && d0 < DP) {
+            qr[u][e4] = load8<T>(qp + (quad * 4 + e4) * a.ldq, d0, D, p.vec_q);
+            dr[u][e4] = load8<T>(dp + (quad * 4 + e4) * ldo, d0, D, p.vec_do);
+          }
+        }
+      }
+      if ((int)threadIdx.x < BR) {
+        const int64_t at = (int64_t)(s.q0 + q0 + min((int)threadIdx.x, n - 1)) * a.H + head;
+        const bool in = (int)threadIdx.x < n;
+        rv[0] = in ? p.row_a[at] : INFINITY;  // p = 0
+        rv[1] = BIAS && in ? p.row_c[at] : 0.0f;
+        rv[2] = in ? p.row_delta[at] : 0.0f;
+      }
+    };
+    const auto fetch_buckets = [&](int i) {
+      const int q0 = (i % rtiles) * BR, n = min(BR, s.nq - q0);
+#pragma unroll
+      for (int x = 0; x < XT; ++x) {
+        const int r = x * 16 + g * 4 + (col & 3);
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          bk[t][x] = 0xFFFFFFFFu;
+          const int64_t j = kt0 + (wave * KT + t) * 16 + (col & 12);
+          if (dist != nullptr && r < n && j < s.nk)
+            bk[t][x] = load_buckets(dist + (int64_t)(q0 + r) * s.nk, (int)j, s.nk);
+        }
+      }
+    };
+    const int total = rtiles * grp;
+    if (total > 0) {
+      if (AHEAD) fetch(0);
+      if (BIAS) fetch_buckets(0);
+    }
+    for (int it = 0; it < total; ++it) {
+      const int n = min(BR, s.nq - (it % rtiles) * BR);
+      if (!AHEAD) fetch(it);
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < RU; ++u) {
+        const int c = u * THREADS + threadIdx.x, quad = c % (BR / 4), d0 = (c / (BR / 4)) * 8;
+        if (d0 < DP) {
+          const int place = interleaved_quad(quad);
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            put8<T>(Qs + (quad * 4 + e4) * LDK + d0, qr[u][e4]);
+            put8<T>(Os + (quad * 4 + e4) * LDK + d0, dr[u][e4]);
+          }
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            x4_t<T> w, y;
+#pragma unroll
+            for (int e4 = 0; e4 < 4; ++e4) {
+              w[e4] = qr[u][e4][e];
+              y[e4] = dr[u][e4][e];
+            }
+            *reinterpret_cast<x4_t<T>*>(Qt + (d0 + e) * LDT + place) = w;
+            *reinterpret_cast<x4_t<T>*>(Ot + (d0 + e) * LDT + place) = y;
+          }
+        }
+      }
+      if ((int)threadIdx.x < BR) {
+        rows[0][threadIdx.x] = rv[0];
+        if (BIAS) rows[1][threadIdx.x] = rv[1];
+        rows[2][threadIdx.x] = rv[2];
+      }
+      __syncthreads();
+      const float* th = tab + (it / rtiles) * (a.B + 1);
+      if (AHEAD && it + 1 < total) fetch(it + 1);
+      if (idle) continue;
+#pragma unroll
+      for (int x2 = 0; x2 < XT / 2; ++x2) {
+        if (x2 * 32 >= n) break;
+        f32x4 sc[KT][2], dp[KT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int x = 2 * x2 + h;
+#pragma unroll
+          for (int t = 0; t < KT; ++t) sc[t][h] = dp[t][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int c = 0; c < KC; ++c) {
+            const frag_t<T, DP> qf = lds_frag<T, DP>(Qs + (x * 16 + col) * LDK, c, g);
+            const frag_t<T, DP> of = lds_frag<T, DP>(Os + (x * 16 + col) * LDK, c, g);
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+              sc[t][h] = mma(qf, kf[t][c], sc[t][h]);
+              dp[t][h] = mma(of, vf[t][c], dp[t][h]);
+            }
+          }
+          const f32x4 ra = *reinterpret_cast<const f32x4*>(&rows[0][x * 16 + g * 4]);
+          const f32x4 rc = BIAS ? *reinterpret_cast<const f32x4*>(&rows[1][x * 16 + g * 4]) : ra;
+          const f32x4 dl = *reinterpret_cast<const f32x4*>(&rows[2][x * 16 + g * 4]);
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+            const unsigned b4 = BIAS ? transpose_quad(bk[t][x], (unsigned)(col & 3)) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const unsigned b = BIAS ? min((b4 >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
+              const float add = BIAS ? th[b] : 0.0f;
+              float slope;
+              const float u = score<T, BIAS, CAP>(sc[t][h][i], add, sx, &slope);
+              float e = weight<BIAS>(u, sx.unit, ra[i], rc[i]);
+              float ds = e * (dp[t][h][i] - dl[i]) * slope;
+              if (BIAS) {  // (columns past the keys: zeros in k, not written)
+                e = add == -INFINITY ? 0.0f : e;
+                ds = add == -INFINITY ? 0.0f : ds;
+              }
+              sc[t][h][i] = e;
+              dp[t][h][i] = ds;
+            }
+          }
+        }
+        x8_t<T> pf[KT], sf[KT];
+#pragma unroll
+        for (int t = 0; t < KT; ++t) {
+          pf[t] = as_operand<T>(sc[t][0], sc[t][1]);
+          sf[t] = as_operand<T>(dp[t][0], dp[t][1]);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const x8_t<T> of = lds8<T>(Ot + (d * 16 + col) * LDT + x2 * 32 + g * 8);
+          const x8_t<T> qf = lds8<T>(Qt + (d * 16 + col) * LDT + x2 * 32 + g * 8);
+#pragma unroll
+          for (int t = 0; t < KT; ++t) {
+            dv[t][d] = mma(of, pf[t], dv[t][d]);
+            dk[t][d] = mma(qf, sf[t], dk[t][d]);
+          }
+        }
+      }
+      if (BIAS && it + 1 < total) fetch_buckets(it + 1);
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      if (key[t] < 0) continue;
+      const int64_t at = ((int64_t)(s.k0 + key[t]) * a.Hk + kvh) * D;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        store4<T>(static_cast<T*>(p.dk) + at, d * 16 + g * 4, D, p.vec_dk, dk[t][d] * a.scale);
+        store4<T>(static_cast<T*>(p.dv) + at, d * 16 + g * 4, D, p.vec_dv, dv[t][d]);
+      }
+    }
+  }
+}
+
+// Tiles of rows the first pass takes.
+struct RowPlan {
+  int waves, qt, copies;
+  int64_t slots;
+};
+inline size_t bins_bytes(int waves, int copies, int64_t B) {
+  return sizeof(float) * (size_t)waves * copies * (B + 1) * kWave;
+}
+
+template <typename T, int DP, int WAVES, int QT>
+int launch_grad_q(const AttnGrad& p, int64_t slots, hipStream_t s) {
+  const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
+  if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
+  const size_t lds = bias_table_bytes(p.a) + (p.bias_part != nullptr ? bins_bytes(WAVES, p.copies, p.a.B) : 0);
+  const bool cap = p.a.cap > 0.0f;
+  const unsigned n = (unsigned)blocks;
+  if (p.a.B > 0) {
+    if (cap) attn_grad_q<T, DP, WAVES, QT, true, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+  } else {
+    if (cap) attn_grad_q<T, DP, WAVES, QT, false, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+  }
+  TFG_LAUNCHED("attn_grad_q");
+  return TFG_OK;
+}
+template <typename T, int DP, int WAVES, int KT>
+int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
+  const int64_t blocks = ((int64_t)p.a.Nk / (WAVES * KT * 16) + p.a.G) * ((p.a.Hk + p.heads - 1) / p.heads);
+  if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many key tiles");
+  const size_t lds = bias_table_bytes(p.a);
+  const bool cap = p.a.cap > 0.0f;
+  const unsigned n = (unsigned)blocks;
+  if (p.a.B > 0) {
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, true, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+  } else {
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, false, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+  }
+  TFG_LAUNCHED("attn_grad_kv");
+  return TFG_OK;
+}
+
+template <typename T, int DP>
+int launch_grad_width(const AttnGrad& p, const RowPlan& r, hipStream_t s) {
+  if (p.a.Nq > 0) {
+    int rc;
+    if (r.qt == 2) rc = launch_grad_q<T, DP, 4, 2>(p, r.slots, s);
+    else if (r.waves == 4) rc = launch_grad_q<T, DP, 4, 1>(p, r.slots, s);
+    else rc = launch_grad_q<T, DP, 1, 1>(p, r.slots, s);
+    if (rc) return rc;
+  }
+  if (p.a.Nk == 0) return TFG_OK;
+  if (DP * sizeof(T) < 512 && p.a.Nk / p.a.G > 192) return launch_grad_kv<T, DP, 4, 2>(p, s);
+  return launch_grad_kv<T, DP, 4, 1>(p, s);
+}
+
+template <typename T>
+int launch_grad_type(AttnGrad& p, const RowPlan& r, hipStream_t s) {
+  const int D = p.a.D;
+  const int64_t ldo = (int64_t)p.a.H * D, ldk = (int64_t)p.a.Hk * D;
+  p.vec_q = row_vector<T>(p.q, p.a.ldq, D);
+  p.vec_k = row_vector<T>(p.k, p.a.ldk, D);
+  p.vec_v = row_vector<T>(p.v, p.a.ldv, D);
+  p.vec_o = row_vector<T>(p.out, ldo, D);
+  p.vec_do = row_vector<T>(p.dout, ldo, D);
+  p.vec_dq = row_vector<T>(p.dq, ldo, D);
+  p.vec_dk = row_vector<T>(p.dk, ldk, D);
+  p.vec_dv = row_vector<T>(p.dv, ldk, D);
+  p.heads = 1;
+  if (D <= 16) return launch_grad_width<T, 16>(p, r, s);
+  if (D <= 32) return launch_grad_width<T, 32>(p, r, s);
+  if (D <= 64) return launch_grad_width<T, 64>(p, r, s);
+  return launch_grad_width<T, 128>(p, r, s);
+}
+
+int launch_grad_bf16(AttnGrad& p, const RowPlan& r, hipStream_t s);
+int launch_grad_f32(AttnGrad& p, const RowPlan& r, hipStream_t s);
+
+}  // namespace tfg

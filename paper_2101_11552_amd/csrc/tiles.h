@@ -49,6 +49,18 @@ __device__ __forceinline__ f32x4 mma(f32x8 a, f32x8 b, f32x4 c) {
   return c;
 }
 
+// Heads of at most 16 columns: a 16 x 16 by 16 x 16 step, four consecutive k a lane.
+__device__ __forceinline__ f32x4 mma(bf16x4 a, bf16x4 b, f32x4 c) {
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a),
+                                                   __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(f32x4 a, f32x4 b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
 // Rounded to nearest even.
 template <typename T> __device__ __forceinline__ T to_type(float x) { return (T)x; }
 
@@ -147,6 +159,44 @@ __device__ __forceinline__ void put8(T* p, x8_t<T> v) {
 // Columns added to an LDS row so that the rows of a 16-lane read start in
 // different banks.
 template <typename T> constexpr int lds_pad() { return 16 / (int)sizeof(T); }
+
+// A lane's part of a head's DP columns as an operand: KC chunks of 32 (of 16 for DP =
+// 16), eight (four) consecutive columns of each.
+template <typename T, int DP> struct Frag {
+  static constexpr int N = DP == 16 ? 4 : 8, KC = DP == 16 ? 1 : DP / 32, W = 4 * N;
+  typedef T type __attribute__((ext_vector_type(N)));
+};
+template <typename T, int DP> using frag_t = typename Frag<T, DP>::type;
+
+template <typename T, int DP>
+__device__ __forceinline__ frag_t<T, DP> zero_frag() {
+  frag_t<T, DP> v;
+#pragma unroll
+  for (int e = 0; e < Frag<T, DP>::N; ++e) v[e] = (T)0.0f;
+  return v;
+}
+// Chunk c of lane group g of a row of D columns in memory (see load8).
+template <typename T, int DP>
+__device__ __forceinline__ frag_t<T, DP> load_frag(const T* row, int c, int g, int D, int vec) {
+  if constexpr (DP == 16) {
+    frag_t<T, DP> v = zero_frag<T, DP>();
+    const int d0 = g * 4;
+    if (d0 >= D) return v;
+    if (vec > 1) return *reinterpret_cast<const frag_t<T, DP>*>(row + d0);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d0 + e < D) v[e] = row[d0 + e];
+    return v;
+  } else {
+    return load8<T>(row, c * 32 + g * 8, D, vec);
+  }
+}
+// The same of a row in LDS.
+template <typename T, int DP>
+__device__ __forceinline__ frag_t<T, DP> lds_frag(const T* row, int c, int g) {
+  if constexpr (DP == 16) return *reinterpret_cast<const frag_t<T, DP>*>(row + g * 4);
+  else return lds8<T>(row + c * 32 + g * 8);
+}
 
 // Two result tiles (a = 0, 1) as one operand of 32 k.
 template <typename T>
