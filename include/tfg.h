@@ -624,7 +624,7 @@ int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int
  * Values of masked pairs' keys are never part of a score; v is weighted by 0
  * there, so that a non-finite v does reach the other rows of its graph and head.
  * q: [Nq, H*D] with leading dimension ldq; k, v: [Nk, kv_heads*D] with ldk, ldv
- * (columns of one projection may be passed in place); D <= 128, H <= 1024, H /
+ * (columns of one projection may be passed in place; below 2^23); D <= 128, H <= 1024, H /
  * kv_heads * B <= 4096. out: [Nq, H*D]; lse: NULL or [Nq, H] float32, log of the sum of
  * exp(u). Rows outside every graph are left as they were.
  * Where there are few queries and many keys, the keys are split over blocks and

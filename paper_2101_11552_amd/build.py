@@ -15,11 +15,15 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libtfg.so")
-SOURCES = ["csr.hip", "norm.hip", "aggregate.hip", "slots_sum.hip", "slots_max.hip",
+# (the longest to compile first)
+SOURCES = ["attention_grad_f32_wide.hip", "attention_grad_bf16_wide.hip",
+           "attention_grad_f32_narrow.hip", "attention_grad_bf16_narrow.hip",
+           "attention_f32_wide.hip", "attention_bf16_wide.hip",
+           "attention_f32_narrow.hip", "attention_bf16_narrow.hip",
+           "csr.hip", "norm.hip", "aggregate.hip", "slots_sum.hip", "slots_max.hip",
            "slots_heads.hip", "slots_masked.hip", "softmax.hip",
            "gat.hip", "gat_dot.hip", "pool.hip", "batch.hip", "backward.hip",
-           "embed.hip", "group_norm.hip", "attention.hip", "attention_bf16.hip", "attention_f32.hip", "attention_grad.hip",
-           "attention_grad_bf16.hip", "attention_grad_f32.hip", "api.cpp"]
+           "embed.hip", "group_norm.hip", "attention.hip", "attention_grad.hip", "api.cpp"]
 # measurement probes for the benchmark (include/tfg_probe.h), a library of their own
 PROBE_LIB = os.path.join(HERE, "libtfg_probe.so")
 PROBE_SOURCES = ["probe.hip"]
@@ -29,6 +33,8 @@ FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
     # keep the compiler from emitting packed-fp32 arithmetic
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+    # matrix products keep their sums in ordinary registers, where the softmax reads them
+    "-mllvm", "-amdgpu-mfma-vgpr-form=1",
     "-I", os.path.join(ROOT, "include"),
 ]
 

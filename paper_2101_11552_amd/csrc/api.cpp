@@ -1006,6 +1006,8 @@ int check_attention(const AttnShape& a, int float_type, int64_t Nq, int64_t Nk, 
   if (D < 1 || D > max_attention_width()) return fail(TFG_ERR_INVALID_ARG, "need 1 <= D <= 128");
   if (a.ldq < H * D || a.ldk < Hk * D || a.ldv < Hk * D)
     return fail(TFG_ERR_INVALID_ARG, "a leading dimension below the row's width");
+  if (a.ldq >= (int64_t(1) << 23) || a.ldk >= (int64_t(1) << 23) || a.ldv >= (int64_t(1) << 23))
+    return fail(TFG_ERR_TOO_LARGE, "a leading dimension not below 2^23");
   if (!(a.cap >= 0.0f) || a.cap > 3.4e38f) return fail(TFG_ERR_INVALID_ARG, "bad cap");
   if (B < 0 || B > 255) return fail(TFG_ERR_INVALID_ARG, "need 0 <= B <= 255");
   if (H / Hk * B > max_attention_bias_entries())

@@ -2,6 +2,8 @@
 // gradient kernels share (gfx950).
 #pragma once
 
+#include <type_traits>
+
 #include "spans.h"
 #include "tiles.h"
 
@@ -57,13 +59,17 @@ __device__ __forceinline__ unsigned load_buckets(const uint8_t* row, int j, int 
   return v;
 }
 
-// tanh. bf16 features: 1 - 2 / (1 + exp(2 x)) on the hardware's exponential and
-// reciprocal; its absolute error of some 2^-22 is far below the features' rounding.
+// f * tanh(x * to_tanh) + add, with to_exp = 2 log2(e) to_tanh.
+// bf16 features: f + add - 2 f / (1 + exp(2 x to_tanh)) on the hardware's exponential
+// and reciprocal, add given with f in it; the tanh's absolute error of some 2^-22 is
+// far below the features' rounding.
 // float32 features: below 0.65 the odd polynomial x + x z P(z), z = x^2, P fitted to
 // (tanh(x) / x - 1) / z for the least relative error (8e-8 with its roundings), above it
 // the same form, whose error is a step or two there.
-template <typename T> __device__ __forceinline__ float cap_tanh(float x) {
+template <typename T>
+__device__ __forceinline__ float capped(float x, float to_tanh, float to_exp, float f, float add) {
   if constexpr (sizeof(T) == 4) {
+    x *= to_tanh;
     const float z = x * x;
     float q = -0.005528633017092943f;
     q = __builtin_fmaf(q, z, 0.020483314990997314f);
@@ -73,22 +79,25 @@ template <typename T> __device__ __forceinline__ float cap_tanh(float x) {
     const float low = __builtin_fmaf(x * z, q, x);
     const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.0f * kLog2e));
     const float high = __builtin_copysignf(1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e), x);
-    return fabsf(x) < 0.65f ? low : high;  // (NaN: high, NaN)
+    return __builtin_fmaf(f, fabsf(x) < 0.65f ? low : high, add);  // (NaN: high, NaN)
   } else {
-    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(1.0f + e);
+    return __builtin_fmaf(-2.0f * f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * to_exp)), add);
   }
 }
+// What `add` carries beside the bias.
+template <typename T> __device__ __forceinline__ float cap_offset(float f) {
+  return sizeof(T) == 2 ? f : 0.0f;
+}
 
-// The biases of the group's heads to LDS, B + 1 a head: bucket B and above are
-// masked, -inf.
+// The biases of the group's heads to LDS, plus `offset`, B + 1 a head: bucket B and
+// above are masked, -inf.
 template <typename T>
-__device__ __forceinline__ void load_bias(const AttnShape& a, int kvh, int grp, float* tab,
-                                          int threads, int tid) {
+__device__ __forceinline__ void load_bias(const AttnShape& a, int kvh, int grp, float offset,
+                                          float* tab, int threads, int tid) {
   const T* b = static_cast<const T*>(a.bias) + (int64_t)kvh * grp * a.B;
   for (int i = tid; i < grp * (a.B + 1); i += threads) {
     const int h = i / (a.B + 1), j = i - h * (a.B + 1);
-    tab[i] = j < a.B ? (float)b[h * a.B + j] : -INFINITY;
+    tab[i] = j < a.B ? (float)b[h * a.B + j] + offset : -INFINITY;
   }
 }
 inline size_t bias_table_bytes(const AttnShape& a) {
@@ -101,44 +110,64 @@ constexpr float kBoundedCap = 60.0f;
 // Scores beyond this are differences of large numbers: see the kernels.
 constexpr float kHugeScore = 1.0e37f;
 
-// ROWS rows of D columns to LDS (row-major, leading dimension LD), zeros from
-// column D and row n on. at(r): a row's first element.
-template <typename T, int ROWS, int DP, int LD, int THREADS, typename At>
-__device__ __forceinline__ void stage_rows(T* dst, int n, int D, int vec, At at) {
-  constexpr int C = DP / 8;
-  for (int c = threadIdx.x; c < ROWS * C; c += THREADS) {
-    const int r = c / C, d0 = (c % C) * 8;
+// Eight columns from d0 on of the row at element `at` past base (the same in every lane).
+// VEC 8: D is a multiple of 16 bytes, the row of one element (16-byte loads at any
+// address); 4: as row_vector says. Columns past D are read from the row's last ones: finite
+// where the row is, and the other operand of their product is zero.
+template <typename T, int VEC>
+__device__ __forceinline__ x8_t<T> load8_within(const T* base, unsigned at, int d0, int D) {
+  if constexpr (VEC == 8 && sizeof(T) == 2) {
+    typedef bf16x8 any8 __attribute__((aligned(2)));
+    return *reinterpret_cast<const any8*>(base + (at + min(d0, D - 8)));
+  } else if constexpr (VEC >= 4) {
+    typedef x4_t<T> any4 __attribute__((aligned(sizeof(T))));
+    const x4_t<T> lo = *reinterpret_cast<const any4*>(base + (at + min(d0, D - 4)));
+    const x4_t<T> hi = *reinterpret_cast<const any4*>(base + (at + min(d0 + 4, D - 4)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else {
     x8_t<T> v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (T)0.0f;
-    if (r < n) v = load8<T>(at(r), d0, D, vec);
-    put8<T>(dst + r * LD + d0, v);
+    for (int e = 0; e < 8; ++e) v[e] = base[at + min(d0 + e, D - 1)];
+    return v;
+  }
+}
+// Whether a kernel's loads may be VEC = 8: a choice for the whole kernel, since a branch
+// around loads would make every tile wait for them.
+template <typename T> inline bool whole_vectors(int D) { return D % (16 / (int)sizeof(T)) == 0; }
+
+// Calls f with the vector length as a constant: 8, or (VEC 0) by the width, where each tile
+// waits for its loads.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void with_vector(int D, F f) {
+  if constexpr (VEC == 8) {
+    f(std::integral_constant<int, 8>{});
+  } else {
+    if (D % 4 == 0) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 1>{});
   }
 }
 
-// ROWS rows to LDS as columns: dst[d][place of the row], places interleaved (see
-// tiles.h), and with nat also row-major there.
-template <typename T, int ROWS, int DP, int LDT, int LD, int THREADS, typename At>
-__device__ __forceinline__ void stage_columns(T* dst, T* nat, int n, int D, int vec, At at) {
-  constexpr int Q = ROWS / 4;
-  for (int c = threadIdx.x; c < Q * (DP / 8); c += THREADS) {
-    const int quad = c % Q, d0 = (c / Q) * 8;
-    x8_t<T> v[4];
+// A thread's units of a tile of ROWS rows: unit c is eight columns of row row8(c), or of
+// the four rows of quad(c).
+template <int ROWS, int DP>
+struct Units {
+  static constexpr int C = DP / 8;
+  static __device__ __forceinline__ int row8(int c) { return c / C; }
+  static __device__ __forceinline__ int col8(int c) { return (c % C) * 8; }
+  static __device__ __forceinline__ int quad(int c) { return c % (ROWS / 4); }
+  static __device__ __forceinline__ int quad_col(int c) { return (c / (ROWS / 4)) * 8; }
+};
+
+// Four rows of eight columns to LDS as columns, places interleaved (see tiles.h).
+template <typename T, int LD>
+__device__ __forceinline__ void put_columns(T* dst, int quad, int d0, const x8_t<T> (&v)[4]) {
+  const int place = interleaved_quad(quad);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+  for (int e = 0; e < 8; ++e) {
+    x4_t<T> w;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = (T)0.0f;
-      if (quad * 4 + i < n) v[i] = load8<T>(at(quad * 4 + i), d0, D, vec);
-      if (nat != nullptr) put8<T>(nat + (quad * 4 + i) * LD + d0, v[i]);
-    }
-    const int place = interleaved_quad(quad);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x4_t<T> w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = v[i][e];
-      *reinterpret_cast<x4_t<T>*>(dst + (d0 + e) * LDT + place) = w;
-    }
+    for (int i = 0; i < 4; ++i) w[i] = v[i][e];
+    *reinterpret_cast<x4_t<T>*>(dst + (d0 + e) * LD + place) = w;
   }
 }
 

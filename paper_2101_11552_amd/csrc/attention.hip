@@ -13,7 +13,7 @@ int key_parts(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk) {
   const int64_t tile = rows <= 16 ? 16 : rows <= 192 ? 64 : 128;
   const int64_t blocks = G * ((rows + tile - 1) / tile) * Hk;
   const int64_t keys = Nk / G;
-  return (int)std::max<int64_t>(std::min<int64_t>({1024 / std::max<int64_t>(blocks, 1), keys / 256, 64}), 1);
+  return (int)std::max<int64_t>(std::min<int64_t>({1024 / std::max<int64_t>(blocks, 1), keys / 256, kKeyParts}), 1);
 }
 
 }  // namespace
@@ -39,7 +39,9 @@ int launch_attention(const AttnShape& a, int float_type, const void* q, const vo
     p.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) +
                                          align_up(sizeof(float) * (size_t)p.nsplit * a.Nq * a.H * a.D, 256));
   }
-  return float_type == TFG_BF16 ? launch_fwd_bf16(p, s) : launch_fwd_f32(p, s);
+  const bool narrow = a.D <= 32;
+  if (float_type == TFG_BF16) return narrow ? launch_fwd_bf16_narrow(p, s) : launch_fwd_bf16_wide(p, s);
+  return narrow ? launch_fwd_f32_narrow(p, s) : launch_fwd_f32_wide(p, s);
 }
 
 namespace {

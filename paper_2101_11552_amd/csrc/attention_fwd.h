@@ -1,5 +1,6 @@
 // Attention inside each graph of a BatchGraph (gfx950), the forward kernels,
-// compiled per type in attention_bf16.hip and attention_f32.hip.
+// compiled per type and
+// width in attention_bf16_narrow.hip and its like.
 //
 //   s = scale * <q, k>;  u = cap * tanh(s / cap) (cap > 0) + bias[head, dist];
 //   out = sum over the graph's unmasked keys of softmax(u) * v
@@ -17,6 +18,8 @@
 // output's own rounding).
 #pragma once
 
+#include <type_traits>
+
 #include "attention.h"
 
 namespace tfg {
@@ -26,7 +29,7 @@ struct AttnFwd {
   const void *q, *k, *v;
   void* out;
   float* lse;
-  int vec_q, vec_k, vec_v, vec_o;
+  int vec_q, vec_o;
   int nsplit;      // > 1: the keys of a graph in that many parts, joined afterwards
   float* part;     // [nsplit][Nq * H][D] unnormalised partial outputs
   float* part_ml;  // [nsplit][Nq * H][2] their maximum and sum
@@ -34,16 +37,18 @@ struct AttnFwd {
   int heads;       // key/value heads a block takes
 };
 
-template <typename T, int DP, int WAVES, int QT, bool BIAS, bool CAP>
+// CAP: 0 none, 1 capped scores, 2 bounded ones (capped at kBoundedCap at most, no bias).
+template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, int CAP>
 __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDV = BN + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
+  using U = Units<BN, DP>;
   // staging units of a thread: rows of eight columns (K), four rows of eight (V)
   constexpr int KU = (BN * DP / 8 + THREADS - 1) / THREADS;
   constexpr int VU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
   // the next tile waits in registers where it takes at most 48 of them
-  constexpr bool AHEAD = (KU * 8 + VU * 32) * sizeof(T) / 4 <= 48;
+  constexpr bool AHEAD = VEC == 8 && (KU * 8 + VU * 32) * sizeof(T) / 4 <= 48;
   __shared__ T Ks[BN * LDK];
   __shared__ T Vt[DP * LDV];
   extern __shared__ float tab[];
@@ -64,8 +69,9 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   const int t0 = min((int)blockIdx.y * per, tiles), t1 = min(t0 + per, tiles);
   const bool flip = a.scale < 0.0f;  // the maximum is taken over raw products: q changes sign
   const float scale = fabsf(a.scale), scale2 = scale * kLog2e;
-  const float to_tanh = CAP ? scale / a.cap : 0.0f, cap2 = a.cap * kLog2e;
-  const bool bounded = CAP && !BIAS && a.cap <= kBoundedCap;
+  constexpr bool bounded = CAP == 2;
+  const float to_tanh = CAP ? scale / a.cap : 0.0f, to_exp = to_tanh * (2.0f * kLog2e);
+  const float cap = bounded ? a.cap * kLog2e : a.cap, cap_add = cap_offset<T>(cap);
 
   // this lane's rows (one a query tile)
   int qi[QT], hg[QT];
@@ -80,7 +86,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   for (int kvh = kvh0; kvh < min(kvh0 + p.heads, a.Hk); ++kvh) {
     if (BIAS) {
       __syncthreads();
-      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+      load_bias<T>(a, kvh, grp, CAP ? cap_add : 0.0f, tab, THREADS, threadIdx.x);
     }
     frag_t<T, DP> qf[QT][KC];
 #pragma unroll
@@ -105,28 +111,27 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
     }
     x8_t<T> kr[KU], vr[VU][4];
     unsigned bk[QT][KT];
-    const auto fetch = [&](int kt) {  // the rows of tile kt to registers
-      const int j0 = kt * BN, n = min(BN, s.nk - j0);
+    const auto fetch = [&](int kt) {  // the rows of tile kt to registers; past the last key, its own
+      const int j0 = kt * BN, last = min(BN, s.nk - j0) - 1;
       const T* kp = static_cast<const T*>(p.k) + (int64_t)(s.k0 + j0) * a.ldk + (int64_t)kvh * D;
       const T* vp = static_cast<const T*>(p.v) + (int64_t)(s.k0 + j0) * a.ldv + (int64_t)kvh * D;
+      const unsigned ldk = (unsigned)a.ldk, ldv = (unsigned)a.ldv;
+      with_vector<T, VEC>(D, [&](auto vec) {
 #pragma unroll
-      for (int u = 0; u < KU; ++u) {
-        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) kr[u][e] = (T)0.0f;
-        if (r < n) kr[u] = load8<T>(kp + r * a.ldk, d0, D, p.vec_k);
-      }
-#pragma unroll
-      for (int u = 0; u < VU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) vr[u][i][e] = (T)0.0f;
-          if (quad * 4 + i < n && d0 < DP)
-            vr[u][i] = load8<T>(vp + (quad * 4 + i) * a.ldv, d0, D, p.vec_v);
+        for (int u = 0; u < KU; ++u) {
+          const int c = u * THREADS + threadIdx.x;
+          if (U::row8(c) < BN)
+            kr[u] = load8_within<T, decltype(vec)::value>(kp, min(U::row8(c), last) * ldk, U::col8(c), D);
         }
-      }
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+          const int c = u * THREADS + threadIdx.x;
+          if (U::quad_col(c) >= DP) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            vr[u][i] = load8_within<T, decltype(vec)::value>(vp, min(U::quad(c) * 4 + i, last) * ldv, U::quad_col(c), D);
+        }
+      });
     };
     const auto fetch_buckets = [&](int kt) {
 #pragma unroll
@@ -147,22 +152,13 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
       __syncthreads();  // the last tile has been used
 #pragma unroll
       for (int u = 0; u < KU; ++u) {
-        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
-        if (r < BN) put8<T>(Ks + r * LDK + d0, kr[u]);
+        const int c = u * THREADS + threadIdx.x;
+        if (U::row8(c) < BN) put8<T>(Ks + U::row8(c) * LDK + U::col8(c), kr[u]);
       }
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
-        if (d0 < DP) {
-          const int place = interleaved_quad(quad);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x4_t<T> w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = vr[u][i][e];
-            *reinterpret_cast<x4_t<T>*>(Vt + (d0 + e) * LDV + place) = w;
-          }
-        }
+        const int c = u * THREADS + threadIdx.x;
+        if (U::quad_col(c) < DP) put_columns<T, LDV>(Vt, U::quad(c), U::quad_col(c), vr[u]);
       }
       __syncthreads();
       if (AHEAD && kt + 1 < t1) fetch(kt + 1);
@@ -179,84 +175,89 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
           for (int t = 0; t < QT; ++t) sc[t][x] = mma(kf, qf[t][c], sc[t][x]);
         }
       }
+      // the tile's weights, in place of its products (tail: keys from n on are masked; with a
+      // bias their buckets are)
+      const auto soften = [&](auto tail) {
 #pragma unroll
-      for (int t = 0; t < QT; ++t) {
-        // scores: natural units with a bias, raw products without one, base 2 where bounded
-        if constexpr (BIAS) {
-          const float* th = tab + hg[t] * (a.B + 1);
+        for (int t = 0; t < QT; ++t) {
+          // scores: natural units with a bias, raw products without one, base 2 where bounded
+          if constexpr (BIAS) {
+            const float* th = tab + hg[t] * (a.B + 1);
 #pragma unroll
-          for (int x = 0; x < KT; ++x)
+            for (int x = 0; x < KT; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const unsigned b = min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B);
-              const float add = th[b];
-              // (a select: whatever a masked pair's product is, NaN too, it is masked)
-              const float u = CAP ? __builtin_fmaf(a.cap, cap_tanh<T>(sc[t][x][i] * to_tanh), add)
-                                  : __builtin_fmaf(sc[t][x][i], scale, add);
-              sc[t][x][i] = b == (unsigned)a.B || add == -INFINITY ? -INFINITY : u;
+              for (int i = 0; i < 4; ++i) {
+                const unsigned b = min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B);
+                const float add = th[b];
+                // (a select: whatever a masked pair's product is, NaN too, it is masked)
+                const float u = CAP ? capped<T>(sc[t][x][i], to_tanh, to_exp, cap, add)
+                                    : __builtin_fmaf(sc[t][x][i], scale, add);
+                sc[t][x][i] = add == -INFINITY ? -INFINITY : u;
+              }
+          } else {
+            if constexpr (CAP) {
+#pragma unroll
+              for (int x = 0; x < KT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sc[t][x][i] = capped<T>(sc[t][x][i], to_tanh, to_exp, cap, cap_add);
             }
-        } else {
-          if constexpr (CAP) {
-            const float f = bounded ? cap2 : a.cap;
+            if constexpr (decltype(tail)::value) {
+#pragma unroll
+              for (int x = 0; x < KT; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  if (x * 16 + g * 4 + i >= n) sc[t][x][i] = -INFINITY;
+            }
+          }
+          float sum = 0.0f;
+          if (bounded) {
 #pragma unroll
             for (int x = 0; x < KT; ++x)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) sc[t][x][i] = f * cap_tanh<T>(sc[t][x][i] * to_tanh);
+              for (int i = 0; i < 4; ++i) {
+                sc[t][x][i] = __builtin_amdgcn_exp2f(sc[t][x][i]);
+                sum += sc[t][x][i];
+              }
+            l[t] += sum;
+            continue;
           }
-          if (n < BN) {
+          const float unit = BIAS || CAP ? kLog2e : scale2;  // one unit of a score in base 2
+          float mx = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+            mx = fmaxf(fmaxf(fmaxf(mx, sc[t][x][0]), fmaxf(sc[t][x][1], sc[t][x][2])), sc[t][x][3]);
+          mx = fmaxf(mx, __shfl_xor(mx, 16));
+          mx = fmaxf(mx, __shfl_xor(mx, 32));
+          const float mn = fmaxf(m[t], mx);
+          float base = mn == -INFINITY ? 0.0f : mn;  // (nothing unmasked so far)
+          if (__ballot(mn > m[t]) != 0) {
+            const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * unit);
+            l[t] *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
+            m[t] = mn;
+          }
+          if (BIAS && __ballot(fabsf(base) > kHugeScore) != 0) {
+            // a bias of the type's lowest value: base * log2(e) would overflow
 #pragma unroll
             for (int x = 0; x < KT; ++x)
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (x * 16 + g * 4 + i >= n) sc[t][x][i] = -INFINITY;
+              for (int i = 0; i < 4; ++i) sc[t][x][i] -= base;
+            base = 0.0f;
           }
-        }
-        float sum = 0.0f;
-        if (bounded) {
+          const float off = -base * unit;
 #pragma unroll
           for (int x = 0; x < KT; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              sc[t][x][i] = __builtin_amdgcn_exp2f(sc[t][x][i]);
+              sc[t][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][i], unit, off));
               sum += sc[t][x][i];
             }
           l[t] += sum;
-          continue;
         }
-        const float unit = BIAS || CAP ? kLog2e : scale2;  // one unit of a score in base 2
-        float mx = -INFINITY;
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-          mx = fmaxf(fmaxf(fmaxf(mx, sc[t][x][0]), fmaxf(sc[t][x][1], sc[t][x][2])), sc[t][x][3]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m[t], mx);
-        float base = mn == -INFINITY ? 0.0f : mn;  // (nothing unmasked so far)
-        if (__ballot(mn > m[t]) != 0) {
-          const float alpha = __builtin_amdgcn_exp2f((m[t] - base) * unit);
-          l[t] *= alpha;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) o[t][d] *= alpha;
-          m[t] = mn;
-        }
-        if (BIAS && __ballot(fabsf(base) > kHugeScore) != 0) {
-          // a bias of the type's lowest value: base * log2(e) would overflow
-#pragma unroll
-          for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sc[t][x][i] -= base;
-          base = 0.0f;
-        }
-        const float off = -base * unit;
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            sc[t][x][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][i], unit, off));
-            sum += sc[t][x][i];
-          }
-        l[t] += sum;
-      }
+      };
+      if (!BIAS && n < BN) soften(std::true_type{});
+      else soften(std::false_type{});
       if (BIAS && kt + 1 < t1) fetch_buckets(kt + 1);
 #pragma unroll
       for (int x = 0; x < KT / 2; ++x) {
@@ -301,39 +302,70 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   }
 }
 
-// Joins the parts of each (query, head): one wavefront a row, lanes over the
-// columns. Rows outside every graph are left as they were.
-template <typename T>
+// Joins the parts of each (query, head): W wavefronts a row, lane i of each with part i's
+// maximum and sum; wavefront w of the row adds the outputs of the parts w, w + W, .., two
+// columns a lane. Rows outside every graph are left as they were.
+constexpr int kKeyParts = 64;  // at most
+constexpr int kFewParts = 4;   // one wavefront a row up to these, else four
+template <typename T, int W>
 __global__ __launch_bounds__(kBlock) void attn_join(AttnFwd p) {
+  constexpr int C = kMaxHeadDim / kWave, R = kBlock / kWave / W, N = W == 1 ? kFewParts : kKeyParts / W;
+  __shared__ float part[W][kMaxHeadDim];
   const AttnShape& a = p.a;
-  const int64_t rows = (int64_t)a.Nq * a.H;
-  const int64_t row = (int64_t)blockIdx.x * (kBlock / kWave) + threadIdx.x / kWave;
-  const int q = (int)(row / a.H);
-  if (row >= rows || q < a.qoff[0] || q >= a.qoff[a.G]) return;
-  const int lane = lane_id();
-  float m = -INFINITY;
-  for (int sp = 0; sp < p.nsplit; ++sp)
-    if (p.part_ml[2 * (sp * rows + row) + 1] != 0.0f) m = fmaxf(m, p.part_ml[2 * (sp * rows + row)]);
-  const float base = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, acc[kMaxHeadDim / kWave] = {};
-  for (int sp = 0; sp < p.nsplit; ++sp) {
-    const float lp = p.part_ml[2 * (sp * rows + row) + 1];
-    if (lp == 0.0f) continue;  // (no keys in this part, or none unmasked)
-    const float w = __builtin_amdgcn_exp2f((p.part_ml[2 * (sp * rows + row)] - base) * kLog2e);
-    l += w * lp;
+  const int lane = lane_id(), wave = uniform((int)threadIdx.x / kWave);
+  const int64_t rows = (int64_t)a.Nq * a.H, row = (int64_t)blockIdx.x * R + (W == 1 ? wave : 0);
+  if (row >= rows) return;
+  const int q = (int)(row / a.H), w0 = W == 1 ? 0 : wave;
+  if (q < a.qoff[0] || q >= a.qoff[a.G]) return;
+  float ml = 0.0f, mm = -INFINITY;  // (a part without keys, or none unmasked: l = 0)
+  if (lane < p.nsplit) {
+    ml = p.part_ml[2 * (lane * rows + row) + 1];
+    mm = ml != 0.0f ? p.part_ml[2 * (lane * rows + row)] : -INFINITY;
+  }
+  float x[N][C];
 #pragma unroll
-    for (int c = 0; c < kMaxHeadDim / kWave; ++c)
-      if (c * kWave + lane < a.D) acc[c] += w * p.part[(sp * rows + row) * a.D + c * kWave + lane];
+  for (int i = 0; i < N; ++i) {
+    const int sp = min(w0 + i * W, p.nsplit - 1);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      x[i][c] = p.part[(sp * rows + row) * a.D + min(c * kWave + lane, a.D - 1)];
+  }
+  float m = mm;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  const float w = ml != 0.0f ? __builtin_amdgcn_exp2f((mm - m) * kLog2e) : 0.0f;
+  float l = w * ml, acc[C] = {};
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) l += __shfl_xor(l, o);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float ws = w0 + i * W < p.nsplit ? __shfl(w, (w0 + i * W) & (kWave - 1)) : 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] += ws != 0.0f ? ws * x[i][c] : 0.0f;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  if (p.lse != nullptr && lane == 0 && w0 == 0)
+    p.lse[row] = l == 0.0f ? -INFINITY : m + log2f(l) * kLn2;
+  T* out = static_cast<T*>(p.out) + row * a.D;
+  if constexpr (W == 1) {
 #pragma unroll
-  for (int c = 0; c < kMaxHeadDim / kWave; ++c)
-    if (c * kWave + lane < a.D)
-      static_cast<T*>(p.out)[row * a.D + c * kWave + lane] = to_type<T>(acc[c] * inv);
-  if (p.lse != nullptr && lane == 0) p.lse[row] = l == 0.0f ? -INFINITY : m + log2f(l) * kLn2;
+    for (int c = 0; c < C; ++c)
+      if (c * kWave + lane < a.D) out[c * kWave + lane] = to_type<T>(acc[c] * inv);
+  } else {
+#pragma unroll
+    for (int c = 0; c < C; ++c) part[wave][c * kWave + lane] = acc[c];
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d < a.D) {
+      float t = part[0][d];
+#pragma unroll
+      for (int j = 1; j < W; ++j) t += part[j][d];
+      out[d] = to_type<T>(t * inv);
+    }
+  }
 }
 
-template <typename T, int DP, int WAVES, int QT>
+template <typename T, int DP, int WAVES, int QT, int VEC>
 int launch_fwd(AttnFwd& p, hipStream_t s) {
   constexpr int BM = WAVES * QT * 16;
   const int grp = p.a.H / p.a.Hk;
@@ -342,46 +374,53 @@ int launch_fwd(AttnFwd& p, hipStream_t s) {
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
   const dim3 grid((unsigned)blocks, (unsigned)p.nsplit);
   const size_t lds = bias_table_bytes(p.a);
-  const bool cap = p.a.cap > 0.0f;
+  const int cap = p.a.cap <= 0.0f ? 0 : p.a.B > 0 || p.a.cap > kBoundedCap ? 1 : 2;
   if (p.a.B > 0) {
-    if (cap) attn_fwd<T, DP, WAVES, QT, true, true><<<grid, WAVES * kWave, lds, s>>>(p);
-    else attn_fwd<T, DP, WAVES, QT, true, false><<<grid, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_fwd<T, DP, WAVES, QT, VEC, true, 1><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, VEC, true, 0><<<grid, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap) attn_fwd<T, DP, WAVES, QT, false, true><<<grid, WAVES * kWave, lds, s>>>(p);
-    else attn_fwd<T, DP, WAVES, QT, false, false><<<grid, WAVES * kWave, lds, s>>>(p);
+    if (cap == 2) attn_fwd<T, DP, WAVES, QT, VEC, false, 2><<<grid, WAVES * kWave, lds, s>>>(p);
+    else if (cap) attn_fwd<T, DP, WAVES, QT, VEC, false, 1><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, VEC, false, 0><<<grid, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_fwd");
   if (p.nsplit > 1) {
     const int64_t rows = (int64_t)p.a.Nq * p.a.H;
-    attn_join<T><<<(unsigned)((rows + 3) / 4), kBlock, 0, s>>>(p);
+    if (p.nsplit <= kFewParts) attn_join<T, 1><<<(unsigned)((rows + 3) / 4), kBlock, 0, s>>>(p);
+    else attn_join<T, 4><<<(unsigned)rows, kBlock, 0, s>>>(p);
     TFG_LAUNCHED("attn_join");
   }
   return TFG_OK;
 }
 
+// Tiles of rows: 128 where graphs have many, 64, or 16 for a few queries each.
 template <typename T, int DP>
 int launch_fwd_rows(AttnFwd& p, hipStream_t s) {
   const int64_t rows = (int64_t)p.a.Nq * (p.a.H / p.a.Hk) / std::max(p.a.G, 1);
-  if (rows <= 16) return launch_fwd<T, DP, 1, 1>(p, s);
-  if (rows <= 192) return launch_fwd<T, DP, 4, 1>(p, s);
-  return launch_fwd<T, DP, 4, 2>(p, s);
-}
-
-template <typename T>
-int launch_fwd_type(AttnFwd& p, hipStream_t s) {
   const int D = p.a.D;
   p.vec_q = row_vector<T>(p.q, p.a.ldq, D);
-  p.vec_k = row_vector<T>(p.k, p.a.ldk, D);
-  p.vec_v = row_vector<T>(p.v, p.a.ldv, D);
   p.vec_o = row_vector<T>(p.out, (int64_t)p.a.H * D, D);
   p.heads = 1;
-  if (D <= 16) return launch_fwd_rows<T, 16>(p, s);
-  if (D <= 32) return launch_fwd_rows<T, 32>(p, s);
-  if (D <= 64) return launch_fwd_rows<T, 64>(p, s);
-  return launch_fwd_rows<T, 128>(p, s);
+  if (!whole_vectors<T>(D))
+    return rows <= 16 ? launch_fwd<T, DP, 1, 1, 0>(p, s) : launch_fwd<T, DP, 4, 1, 0>(p, s);
+  if (rows <= 16) return launch_fwd<T, DP, 1, 1, 8>(p, s);
+  if (rows <= 192) return launch_fwd<T, DP, 4, 1, 8>(p, s);
+  return launch_fwd<T, DP, 4, 2, 8>(p, s);
 }
 
-int launch_fwd_bf16(AttnFwd& p, hipStream_t s);
-int launch_fwd_f32(AttnFwd& p, hipStream_t s);
+// Heads of at most 32 columns, and wider ones (translation units of their own).
+template <typename T>
+int launch_fwd_narrow(AttnFwd& p, hipStream_t s) {
+  return p.a.D <= 16 ? launch_fwd_rows<T, 16>(p, s) : launch_fwd_rows<T, 32>(p, s);
+}
+template <typename T>
+int launch_fwd_wide(AttnFwd& p, hipStream_t s) {
+  return p.a.D <= 64 ? launch_fwd_rows<T, 64>(p, s) : launch_fwd_rows<T, 128>(p, s);
+}
+#define TFG_ATTN_FWD(name) int launch_fwd_##name(AttnFwd& p, hipStream_t s)
+TFG_ATTN_FWD(bf16_narrow);
+TFG_ATTN_FWD(bf16_wide);
+TFG_ATTN_FWD(f32_narrow);
+TFG_ATTN_FWD(f32_wide);
 
 }  // namespace tfg

@@ -1,5 +1,5 @@
 // Gradients of the attention inside each graph of a BatchGraph (gfx950), the
-// kernels, compiled per type in attention_grad_bf16.hip and attention_grad_f32.hip.
+// kernels, compiled per type and width in attention_grad_bf16_narrow.hip and its like.
 //
 // With p = exp(u - lse) formed again from the forward's log-sum and
 // delta[row] = <dout[row], out[row]> (= the sum of p dp over the keys):
@@ -43,30 +43,42 @@ struct AttnGrad {
 constexpr float kLongLse = 4096.0f;
 
 struct ScoreScale {
-  float scale, to_tanh, unit, cap;  // unit: from what score() gives to base 2
+  float scale, to_tanh, to_exp, cap;
+  float add;   // the score's addend without a bias
+  float unit;  // from what score() gives to base 2
 };
-template <bool BIAS, bool CAP>
-__device__ __forceinline__ ScoreScale score_scale(const AttnShape& a) {
-  return ScoreScale{a.scale, CAP ? a.scale / a.cap : 0.0f,
-                    BIAS ? kLog2e : CAP ? a.cap * kLog2e : a.scale * kLog2e, a.cap};
-}
-// A raw product as a score (natural units with a bias, else times unit in base 2)
-// and the cap's derivative there. add: -inf masks, whatever the product is.
 template <typename T, bool BIAS, bool CAP>
-__device__ __forceinline__ float score(float x, float add, const ScoreScale& c, float* slope) {
+__device__ __forceinline__ ScoreScale score_scale(const AttnShape& a) {
+  ScoreScale c;
+  c.scale = a.scale;
+  c.to_tanh = CAP ? a.scale / a.cap : 0.0f;
+  c.to_exp = c.to_tanh * (2.0f * kLog2e);
+  c.cap = a.cap;
+  c.add = CAP ? cap_offset<T>(a.cap) : 0.0f;
+  c.unit = BIAS || CAP ? kLog2e : a.scale * kLog2e;
+  return c;
+}
+// A raw product as a score (natural units with a bias or a cap, the product itself
+// without). add: -inf masks, whatever the product is.
+template <typename T, bool BIAS, bool CAP>
+__device__ __forceinline__ float score(float x, float add, const ScoreScale& c) {
   float u = x;
-  if constexpr (CAP) {
-    const float t = cap_tanh<T>(x * c.to_tanh);
-    *slope = __builtin_fmaf(-t, t, 1.0f);
-    u = t;
-  } else {
-    *slope = 1.0f;
-  }
-  if constexpr (BIAS) {
-    u = __builtin_fmaf(u, CAP ? c.cap : c.scale, add);
-    return add == -INFINITY ? -INFINITY : u;
-  }
+  if constexpr (CAP) u = capped<T>(x, c.to_tanh, c.to_exp, c.cap, add);
+  else if constexpr (BIAS) u = __builtin_fmaf(x, c.scale, add);
+  if constexpr (BIAS) return add == -INFINITY ? -INFINITY : u;
   return u;
+}
+// The cap's derivative 1 - tanh^2 there. bf16: 4 r (1 - r), r = 1 / (1 + exp(2 x)).
+template <typename T, bool CAP>
+__device__ __forceinline__ float cap_slope(float x, const ScoreScale& c) {
+  if constexpr (!CAP) return 1.0f;
+  if constexpr (sizeof(T) == 4) {
+    const float t = capped<T>(x, c.to_tanh, c.to_exp, 1.0f, 0.0f);
+    return __builtin_fmaf(-t, t, 1.0f);
+  } else {
+    const float r = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * c.to_exp));
+    return 4.0f * __builtin_fmaf(-r, r, r);
+  }
 }
 template <bool BIAS>
 __device__ __forceinline__ float weight(float u, float unit, float ra, float rc) {
@@ -74,15 +86,16 @@ __device__ __forceinline__ float weight(float u, float unit, float ra, float rc)
   return __builtin_amdgcn_exp2f(__builtin_fmaf(u, unit, -ra));
 }
 
-template <typename T, int DP, int WAVES, int QT, bool BIAS, bool CAP>
+template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP>
 __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BN + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
+  using U = Units<BN, DP>;
   // staging units of a thread: four rows of eight columns (K), rows of eight (V)
   constexpr int KU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
   constexpr int VU = (BN * (DP / 8) + THREADS - 1) / THREADS;
-  constexpr bool AHEAD = (KU * 32 + VU * 8) * sizeof(T) / 4 <= 48;
+  constexpr bool AHEAD = VEC == 8 && (KU * 32 + VU * 8) * sizeof(T) / 4 <= 48;
   __shared__ T Ks[BN * LDK];
   __shared__ T Vs[BN * LDK];
   __shared__ T Kt[DP * LDT];
@@ -108,7 +121,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
   const int wave = uniform((int)threadIdx.x / kWave);
   const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
   const int tiles = (s.nk + BN - 1) / BN;
-  const ScoreScale sx = score_scale<BIAS, CAP>(a);
+  const ScoreScale sx = score_scale<T, BIAS, CAP>(a);
   int qi[QT], hg[QT];
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
@@ -121,7 +134,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
   for (int kvh = kvh0; kvh < kvh1; ++kvh) {
     if (BIAS) {
       __syncthreads();
-      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+      load_bias<T>(a, kvh, grp, sx.add, tab, THREADS, threadIdx.x);
       if (want_bias)
         for (int i = threadIdx.x; i < WAVES * p.copies * (a.B + 1) * kWave; i += THREADS) bins[i] = 0.0f;
     }
@@ -161,50 +174,42 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 
     x8_t<T> kr[KU][4], vr[VU];
     unsigned bk[QT][KT];
-    const auto fetch = [&](int kt) {
-      const int j0 = kt * BN, n = min(BN, s.nk - j0);
+    const auto fetch = [&](int kt) {  // past the last key, its own row (p = 0 there)
+      const int j0 = kt * BN, last = min(BN, s.nk - j0) - 1;
       const T* kp = static_cast<const T*>(p.k) + (int64_t)(s.k0 + j0) * a.ldk + (int64_t)kvh * D;
       const T* vp = static_cast<const T*>(p.v) + (int64_t)(s.k0 + j0) * a.ldv + (int64_t)kvh * D;
+      const unsigned ldk = (unsigned)a.ldk, ldv = (unsigned)a.ldv;
+      with_vector<T, VEC>(D, [&](auto vec) {
 #pragma unroll
-      for (int u = 0; u < KU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
+        for (int u = 0; u < KU; ++u) {
+          const int c = u * THREADS + threadIdx.x;
+          if (U::quad_col(c) >= DP) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) kr[u][i][e] = (T)0.0f;
-          if (quad * 4 + i < n && d0 < DP)
-            kr[u][i] = load8<T>(kp + (quad * 4 + i) * a.ldk, d0, D, p.vec_k);
+          for (int i = 0; i < 4; ++i)
+            kr[u][i] = load8_within<T, decltype(vec)::value>(kp, min(U::quad(c) * 4 + i, last) * ldk, U::quad_col(c), D);
         }
-      }
 #pragma unroll
-      for (int u = 0; u < VU; ++u) {
-        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) vr[u][e] = (T)0.0f;
-        if (r < n) vr[u] = load8<T>(vp + r * a.ldv, d0, D, p.vec_v);
-      }
+        for (int u = 0; u < VU; ++u) {
+          const int c = u * THREADS + threadIdx.x;
+          if (U::row8(c) < BN)
+            vr[u] = load8_within<T, decltype(vec)::value>(vp, min(U::row8(c), last) * ldv, U::col8(c), D);
+        }
+      });
     };
     const auto place_tile = [&]() {  // the fetched rows to LDS
 #pragma unroll
       for (int u = 0; u < KU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BN / 4), d0 = (c / (BN / 4)) * 8;
-        if (d0 < DP) {
+        const int c = u * THREADS + threadIdx.x;
+        if (U::quad_col(c) < DP) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) put8<T>(Ks + (quad * 4 + i) * LDK + d0, kr[u][i]);
-          const int place = interleaved_quad(quad);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x4_t<T> w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = kr[u][i][e];
-            *reinterpret_cast<x4_t<T>*>(Kt + (d0 + e) * LDT + place) = w;
-          }
+          for (int i = 0; i < 4; ++i) put8<T>(Ks + (U::quad(c) * 4 + i) * LDK + U::quad_col(c), kr[u][i]);
+          put_columns<T, LDT>(Kt, U::quad(c), U::quad_col(c), kr[u]);
         }
       }
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
-        const int c = u * THREADS + threadIdx.x, r = c / (DP / 8), d0 = (c % (DP / 8)) * 8;
-        if (r < BN) put8<T>(Vs + r * LDK + d0, vr[u]);
+        const int c = u * THREADS + threadIdx.x;
+        if (U::row8(c) < BN) put8<T>(Vs + U::row8(c) * LDK + U::col8(c), vr[u]);
       }
     };
     const auto fetch_buckets = [&](int kt) {
@@ -260,8 +265,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const unsigned b = min((b4 >> (8 * i)) & 0xFFu, (unsigned)a.B);
-              float slope;
-              float u = score<T, BIAS, CAP>(sc[t][i], BIAS ? tab[hg[t] * (a.B + 1) + b] : 0.0f, sx, &slope);
+              float u = score<T, BIAS, CAP>(sc[t][i], BIAS ? tab[hg[t] * (a.B + 1) + b] : sx.add, sx);
               if (!BIAS) u = x * 16 + g * 4 + i < n ? u * sx.unit : -INFINITY;
               sc[t][i] = u;
               mx = fmaxf(mx, u);
@@ -342,9 +346,9 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const unsigned b = BIAS ? min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
-              const float add = BIAS ? th[b] : 0.0f;
-              float slope;
-              const float u = score<T, BIAS, CAP>(sc[h][t][i], add, sx, &slope);
+              const float add = BIAS ? th[b] : sx.add;
+              const float u = score<T, BIAS, CAP>(sc[h][t][i], add, sx);
+              const float slope = cap_slope<T, CAP>(sc[h][t][i], sx);
               const bool live = BIAS ? add != -INFINITY : x * 16 + g * 4 + i < n;
               float du = weight<BIAS>(u, sx.unit, ra[t], rc[t]) * (dp[h][t][i] - delta[t]);
               du = live ? du : 0.0f;
@@ -374,18 +378,25 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
     }
     if (!want_bias) continue;
     __syncthreads();
-    // (head, bucket) sums of the bins; neighbouring buckets start at other lanes, so
-    // that they read other banks
+    // (head, bucket) sums of the bins
+    if (p.copies == 1 && 16 % grp == 0) {
+      // one head a lane, col % grp: a wavefront a bucket, the lanes of a head added up
+      for (int b = wave; b < a.B; b += WAVES) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += bins[(w * (a.B + 1) + b) * kWave + lane];
+        for (int o = kWave / 2; o >= grp; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane < grp) p.bias_part[(slot * a.H + (int64_t)kvh * grp + lane) * a.B + b] = sum;
+      }
+      continue;
+    }
     for (int i = threadIdx.x; i < grp * a.B; i += THREADS) {
       const int h = i / a.B, b = i % a.B;
       float sum = 0.0f;
       for (int w = 0; w < WAVES * p.copies; ++w) {
-        // the row of column c in this bin is (w * 16 + c) past the tile's first, up to
-        // a multiple of the group where one bin serves every query tile
-        const int first = p.copies > 1 || QT == 1 ? w * 16 : 0;
-        const int base = (int)((r0 + first) % grp);
+        const int base = (int)((r0 + w * 16) % grp);  // the row of column c is w * 16 + c
         for (int e = 0; e < kWave; ++e) {
-          const int ln = (e + b) & (kWave - 1);
+          const int ln = (e + b) & (kWave - 1);  // (neighbouring buckets: other banks)
           if ((base + (ln & 15)) % grp == h) sum += bins[(w * (a.B + 1) + b) * kWave + ln];
         }
       }
@@ -406,13 +417,14 @@ __device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
   return (lo & 0xFFFFu) | (hi << 16);
 }
 
-template <typename T, int DP, int WAVES, int KT, bool BIAS, bool CAP>
+template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP>
 __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
   constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BR + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, XT = BR / 16;
+  using U = Units<BR, DP>;
   constexpr int RU = (BR / 4 * (DP / 8) + THREADS - 1) / THREADS;  // four rows of eight columns
-  constexpr bool AHEAD = RU * 64 * sizeof(T) / 4 <= 64;
+  constexpr bool AHEAD = VEC == 8 && RU * 64 * sizeof(T) / 4 <= 64;
   __shared__ T Qs[BR * LDK];
   __shared__ T Os[BR * LDK];
   __shared__ T Qt[DP * LDT];
@@ -430,7 +442,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
   const int lane = lane_id(), col = lane & 15, g = lane >> 4;
   const int wave = uniform((int)threadIdx.x / kWave);
   const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
-  const ScoreScale sx = score_scale<BIAS, CAP>(a);
+  const ScoreScale sx = score_scale<T, BIAS, CAP>(a);
   const bool idle = kt0 + wave * (KT * 16) >= s.nk;  // a wavefront without keys only stages
   int key[KT];
 #pragma unroll
@@ -443,7 +455,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
   for (int kvh = kvh0; kvh < min(kvh0 + p.heads, a.Hk); ++kvh) {
     if (BIAS) {
       __syncthreads();
-      load_bias<T>(a, kvh, grp, tab, THREADS, threadIdx.x);
+      load_bias<T>(a, kvh, grp, sx.add, tab, THREADS, threadIdx.x);
     }
     frag_t<T, DP> kf[KT][KC], vf[KT][KC];
 #pragma unroll
@@ -473,19 +485,20 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
       const T* qp = static_cast<const T*>(p.q) + (int64_t)(s.q0 + q0) * a.ldq + (int64_t)head * D;
       const int64_t ldo = (int64_t)a.H * D;
       const T* dp = static_cast<const T*>(p.dout) + (int64_t)(s.q0 + q0) * ldo + (int64_t)head * D;
+      const unsigned ldq = (unsigned)a.ldq, ldd = (unsigned)ldo;
+      with_vector<T, VEC>(D, [&](auto vec) {  // past the last query, its own row (p = 0 there)
 #pragma unroll
-      for (int u = 0; u < RU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BR / 4), d0 = (c / (BR / 4)) * 8;
+        for (int u = 0; u < RU; ++u) {
+          const int c = u * THREADS + threadIdx.x;
+          if (U::quad_col(c) >= DP) continue;
 #pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) qr[u][e4][e] = dr[u][e4][e] = (T)0.0f;
-          if (quad * 4 + e4 < n && d0 < DP) {
-            qr[u][e4] = load8<T>(qp + (quad * 4 + e4) * a.ldq, d0, D, p.vec_q);
-            dr[u][e4] = load8<T>(dp + (quad * 4 + e4) * ldo, d0, D, p.vec_do);
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const int r = min(U::quad(c) * 4 + e4, n - 1);
+            qr[u][e4] = load8_within<T, decltype(vec)::value>(qp, r * ldq, U::quad_col(c), D);
+            dr[u][e4] = load8_within<T, decltype(vec)::value>(dp, r * ldd, U::quad_col(c), D);
           }
         }
-      }
+      });
       if ((int)threadIdx.x < BR) {
         const int64_t at = (int64_t)(s.q0 + q0 + min((int)threadIdx.x, n - 1)) * a.H + head;
         const bool in = (int)threadIdx.x < n;
@@ -519,25 +532,15 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
       __syncthreads();
 #pragma unroll
       for (int u = 0; u < RU; ++u) {
-        const int c = u * THREADS + threadIdx.x, quad = c % (BR / 4), d0 = (c / (BR / 4)) * 8;
-        if (d0 < DP) {
-          const int place = interleaved_quad(quad);
+        const int c = u * THREADS + threadIdx.x;
+        if (U::quad_col(c) < DP) {
 #pragma unroll
           for (int e4 = 0; e4 < 4; ++e4) {
-            put8<T>(Qs + (quad * 4 + e4) * LDK + d0, qr[u][e4]);
-            put8<T>(Os + (quad * 4 + e4) * LDK + d0, dr[u][e4]);
+            put8<T>(Qs + (U::quad(c) * 4 + e4) * LDK + U::quad_col(c), qr[u][e4]);
+            put8<T>(Os + (U::quad(c) * 4 + e4) * LDK + U::quad_col(c), dr[u][e4]);
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x4_t<T> w, y;
-#pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-              w[e4] = qr[u][e4][e];
-              y[e4] = dr[u][e4][e];
-            }
-            *reinterpret_cast<x4_t<T>*>(Qt + (d0 + e) * LDT + place) = w;
-            *reinterpret_cast<x4_t<T>*>(Ot + (d0 + e) * LDT + place) = y;
-          }
+          put_columns<T, LDT>(Qt, U::quad(c), U::quad_col(c), qr[u]);
+          put_columns<T, LDT>(Ot, U::quad(c), U::quad_col(c), dr[u]);
         }
       }
       if ((int)threadIdx.x < BR) {
@@ -577,9 +580,9 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const unsigned b = BIAS ? min((b4 >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
-              const float add = BIAS ? th[b] : 0.0f;
-              float slope;
-              const float u = score<T, BIAS, CAP>(sc[t][h][i], add, sx, &slope);
+              const float add = BIAS ? th[b] : sx.add;
+              const float u = score<T, BIAS, CAP>(sc[t][h][i], add, sx);
+              const float slope = cap_slope<T, CAP>(sc[t][h][i], sx);
               float e = weight<BIAS>(u, sx.unit, ra[i], rc[i]);
               float ds = e * (dp[t][h][i] - dl[i]) * slope;
               if (BIAS) {  // (columns past the keys: zeros in k, not written)
@@ -632,7 +635,7 @@ inline size_t bins_bytes(int waves, int copies, int64_t B) {
   return sizeof(float) * (size_t)waves * copies * (B + 1) * kWave;
 }
 
-template <typename T, int DP, int WAVES, int QT>
+template <typename T, int DP, int WAVES, int QT, int VEC>
 int launch_grad_q(const AttnGrad& p, int64_t slots, hipStream_t s) {
   const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
@@ -640,16 +643,16 @@ int launch_grad_q(const AttnGrad& p, int64_t slots, hipStream_t s) {
   const bool cap = p.a.cap > 0.0f;
   const unsigned n = (unsigned)blocks;
   if (p.a.B > 0) {
-    if (cap) attn_grad_q<T, DP, WAVES, QT, true, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_q<T, DP, WAVES, QT, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, true, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, VEC, true, false><<<n, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap) attn_grad_q<T, DP, WAVES, QT, false, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_q<T, DP, WAVES, QT, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, false, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, VEC, false, false><<<n, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_grad_q");
   return TFG_OK;
 }
-template <typename T, int DP, int WAVES, int KT>
+template <typename T, int DP, int WAVES, int KT, int VEC>
 int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
   const int64_t blocks = ((int64_t)p.a.Nk / (WAVES * KT * 16) + p.a.G) * ((p.a.Hk + p.heads - 1) / p.heads);
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many key tiles");
@@ -657,32 +660,18 @@ int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
   const bool cap = p.a.cap > 0.0f;
   const unsigned n = (unsigned)blocks;
   if (p.a.B > 0) {
-    if (cap) attn_grad_kv<T, DP, WAVES, KT, true, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_kv<T, DP, WAVES, KT, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, true, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, VEC, true, false><<<n, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap) attn_grad_kv<T, DP, WAVES, KT, false, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_kv<T, DP, WAVES, KT, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, false, true><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, VEC, false, false><<<n, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_grad_kv");
   return TFG_OK;
 }
 
 template <typename T, int DP>
-int launch_grad_width(const AttnGrad& p, const RowPlan& r, hipStream_t s) {
-  if (p.a.Nq > 0) {
-    int rc;
-    if (r.qt == 2) rc = launch_grad_q<T, DP, 4, 2>(p, r.slots, s);
-    else if (r.waves == 4) rc = launch_grad_q<T, DP, 4, 1>(p, r.slots, s);
-    else rc = launch_grad_q<T, DP, 1, 1>(p, r.slots, s);
-    if (rc) return rc;
-  }
-  if (p.a.Nk == 0) return TFG_OK;
-  if (DP * sizeof(T) < 512 && p.a.Nk / p.a.G > 192) return launch_grad_kv<T, DP, 4, 2>(p, s);
-  return launch_grad_kv<T, DP, 4, 1>(p, s);
-}
-
-template <typename T>
-int launch_grad_type(AttnGrad& p, const RowPlan& r, hipStream_t s) {
+int launch_grad_width(AttnGrad& p, const RowPlan& r, hipStream_t s) {
   const int D = p.a.D;
   const int64_t ldo = (int64_t)p.a.H * D, ldk = (int64_t)p.a.Hk * D;
   p.vec_q = row_vector<T>(p.q, p.a.ldq, D);
@@ -694,13 +683,33 @@ int launch_grad_type(AttnGrad& p, const RowPlan& r, hipStream_t s) {
   p.vec_dk = row_vector<T>(p.dk, ldk, D);
   p.vec_dv = row_vector<T>(p.dv, ldk, D);
   p.heads = 1;
-  if (D <= 16) return launch_grad_width<T, 16>(p, r, s);
-  if (D <= 32) return launch_grad_width<T, 32>(p, r, s);
-  if (D <= 64) return launch_grad_width<T, 64>(p, r, s);
-  return launch_grad_width<T, 128>(p, r, s);
+  const bool whole = whole_vectors<T>(D);
+  if (p.a.Nq > 0) {
+    int rc;
+    if (r.qt == 2) rc = whole ? launch_grad_q<T, DP, 4, 2, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 2, 0>(p, r.slots, s);
+    else if (r.waves == 4) rc = whole ? launch_grad_q<T, DP, 4, 1, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 1, 0>(p, r.slots, s);
+    else rc = launch_grad_q<T, DP, 1, 1, 0>(p, r.slots, s);
+    if (rc) return rc;
+  }
+  if (p.a.Nk == 0) return TFG_OK;
+  if (!whole) return launch_grad_kv<T, DP, 4, 1, 0>(p, s);
+  if (DP * sizeof(T) < 512 && p.a.Nk / p.a.G > 192) return launch_grad_kv<T, DP, 4, 2, 8>(p, s);
+  return launch_grad_kv<T, DP, 4, 1, 8>(p, s);
 }
 
-int launch_grad_bf16(AttnGrad& p, const RowPlan& r, hipStream_t s);
-int launch_grad_f32(AttnGrad& p, const RowPlan& r, hipStream_t s);
+// Heads of at most 32 columns, and wider ones (translation units of their own).
+template <typename T>
+int launch_grad_narrow(AttnGrad& p, const RowPlan& r, hipStream_t s) {
+  return p.a.D <= 16 ? launch_grad_width<T, 16>(p, r, s) : launch_grad_width<T, 32>(p, r, s);
+}
+template <typename T>
+int launch_grad_wide(AttnGrad& p, const RowPlan& r, hipStream_t s) {
+  return p.a.D <= 64 ? launch_grad_width<T, 64>(p, r, s) : launch_grad_width<T, 128>(p, r, s);
+}
+#define TFG_ATTN_GRAD(name) int launch_grad_##name(AttnGrad& p, const RowPlan& r, hipStream_t s)
+TFG_ATTN_GRAD(bf16_narrow);
+TFG_ATTN_GRAD(bf16_wide);
+TFG_ATTN_GRAD(f32_narrow);
+TFG_ATTN_GRAD(f32_wide);
 
 }  // namespace tfg

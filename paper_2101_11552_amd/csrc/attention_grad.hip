@@ -67,7 +67,10 @@ int launch_attention_backward(const AttnShape& a, int float_type, const void* q,
   p.row_delta = reinterpret_cast<float*>(w + L.delta);
   p.bias_part = dbias != nullptr ? reinterpret_cast<float*>(w + L.part) : nullptr;
   p.copies = r.copies;
-  const int rc = float_type == TFG_BF16 ? launch_grad_bf16(p, r, s) : launch_grad_f32(p, r, s);
+  const bool narrow = a.D <= 32;
+  int rc;
+  if (float_type == TFG_BF16) rc = narrow ? launch_grad_bf16_narrow(p, r, s) : launch_grad_bf16_wide(p, r, s);
+  else rc = narrow ? launch_grad_f32_narrow(p, r, s) : launch_grad_f32_wide(p, r, s);
   if (rc || dbias == nullptr) return rc;
   // (no queries: no rows to add, zeros)
   double* sums = reinterpret_cast<double*>(w + L.sums);
