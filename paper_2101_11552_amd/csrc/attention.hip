@@ -1,6 +1,7 @@
 // Attention inside each graph of a BatchGraph (gfx950): the choice of kernels and the
-// check of offsets. The kernels are in attention_fwd.h.
-#include "attention_fwd.h"
+// check of offsets. The kernels are in attention_fwd.h and
+// attention_small.h.
+#include "attention_launch.h"
 
 namespace tfg {
 namespace {
@@ -8,7 +9,7 @@ namespace {
 // Parts of the keys of each graph: more than one where the rows alone leave most
 // of the card idle and graphs have many keys.
 int key_parts(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk) {
-  if (G < 1 || Nq < 1) return 1;
+  if (G < 1 || Nq < 1 || small_graphs(Nq, Nk, G, Hk)) return 1;
   const int64_t grp = H / Hk, rows = Nq * grp / G;
   const int64_t tile = rows <= 16 ? 16 : rows <= 192 ? 64 : 128;
   const int64_t blocks = G * ((rows + tile - 1) / tile) * Hk;

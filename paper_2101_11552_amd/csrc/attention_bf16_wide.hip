@@ -1,5 +1,5 @@
 // The forward attention kernels for bf16 heads of more than 32 columns.
-#include "attention_fwd.h"
+#include "attention_launch.h"
 
 namespace tfg {
 TFG_ATTN_FWD(bf16_wide) { return launch_fwd_wide<__bf16>(p, s); }

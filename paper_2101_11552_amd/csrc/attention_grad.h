@@ -37,6 +37,8 @@ struct AttnGrad {
   int copies;        // bias bins a wavefront keeps: one, or one a query tile
   int small;         // graphs of at most so many queries and keys are another launch's
   int heads;         // key/value heads a block takes
+  int nsplit;        // > 1: the queries of a key tile in that many parts, joined afterwards
+  float* part;       // [nsplit][2][Nk * Hk * D] partial dk (without scale), dv
 };
 
 // Beyond this log-sum its rounding (2^-24 of it) is felt in exp(u - lse).
@@ -59,13 +61,12 @@ __device__ __forceinline__ ScoreScale score_scale(const AttnShape& a) {
   return c;
 }
 // A raw product as a score (natural units with a bias or a cap, the product itself
-// without). add: -inf masks, whatever the product is.
+// without).
 template <typename T, bool BIAS, bool CAP>
 __device__ __forceinline__ float score(float x, float add, const ScoreScale& c) {
   float u = x;
   if constexpr (CAP) u = capped<T>(x, c.to_tanh, c.to_exp, c.cap, add);
   else if constexpr (BIAS) u = __builtin_fmaf(x, c.scale, add);
-  if constexpr (BIAS) return add == -INFINITY ? -INFINITY : u;
   return u;
 }
 // The cap's derivative 1 - tanh^2 there. bf16: 4 r (1 - r), r = 1 / (1 + exp(2 x)).
@@ -84,6 +85,23 @@ template <bool BIAS>
 __device__ __forceinline__ float weight(float u, float unit, float ra, float rc) {
   if constexpr (BIAS) return __builtin_amdgcn_exp2f(__builtin_fmaf(u - ra, unit, rc));
   return __builtin_amdgcn_exp2f(__builtin_fmaf(u, unit, -ra));
+}
+
+// Four values to a lane's own bins (a column of LDS), in order: all four are read, each is
+// added to what the one before it in the same bin has left, and the last write stays.
+// (LDS additions of floats, ds_add_f32, take some 150 cycles a wavefront here.)
+__device__ __forceinline__ void add_to_bins(float* bin, const unsigned (&b)[4], f32x4 v) {
+  float r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = bin[b[i] * kWave];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int j = 0; j < i; ++j) r[i] = b[j] == b[i] ? r[j] : r[i];
+    r[i] += v[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bin[b[i] * kWave] = r[i];
 }
 
 template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP>
@@ -265,8 +283,10 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const unsigned b = min((b4 >> (8 * i)) & 0xFFu, (unsigned)a.B);
-              float u = score<T, BIAS, CAP>(sc[t][i], BIAS ? tab[hg[t] * (a.B + 1) + b] : sx.add, sx);
-              if (!BIAS) u = x * 16 + g * 4 + i < n ? u * sx.unit : -INFINITY;
+              const float add = BIAS ? tab[hg[t] * (a.B + 1) + b] : sx.add;
+              float u = score<T, BIAS, CAP>(sc[t][i], add, sx);
+              if (BIAS) u = add == -INFINITY ? -INFINITY : u;
+              else u = x * 16 + g * 4 + i < n ? u * sx.unit : -INFINITY;
               sc[t][i] = u;
               mx = fmaxf(mx, u);
             }
@@ -339,24 +359,30 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           const float* th = tab + hg[t] * (a.B + 1);
-          float* bin = bins + (wave * p.copies + (p.copies > 1 ? t : 0)) * (a.B + 1) * kWave + lane;
+          unsigned b[2][4];
+          float add[2][4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int x = 2 * x2 + h;
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const unsigned b = BIAS ? min((bk[t][x] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
-              const float add = BIAS ? th[b] : sx.add;
-              const float u = score<T, BIAS, CAP>(sc[h][t][i], add, sx);
-              const float slope = cap_slope<T, CAP>(sc[h][t][i], sx);
-              const bool live = BIAS ? add != -INFINITY : x * 16 + g * 4 + i < n;
-              float du = weight<BIAS>(u, sx.unit, ra[t], rc[t]) * (dp[h][t][i] - delta[t]);
-              du = live ? du : 0.0f;
-              // (one lane adds to a bin: the order of its additions is the program's)
-              if (want_bias)
-                __hip_atomic_fetch_add(bin + b * kWave, du, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-              sc[h][t][i] = du * slope;
+              b[h][i] = BIAS ? min((bk[t][2 * x2 + h] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
+              add[h][i] = BIAS ? th[b[h][i]] : sx.add;
             }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float u = score<T, BIAS, CAP>(sc[h][t][i], add[h][i], sx);
+              const float slope = cap_slope<T, CAP>(sc[h][t][i], sx);
+              const bool live = BIAS ? add[h][i] != -INFINITY : (2 * x2 + h) * 16 + g * 4 + i < n;
+              const float du = weight<BIAS>(u, sx.unit, ra[t], rc[t]) * (dp[h][t][i] - delta[t]);
+              dp[h][t][i] = live ? du : 0.0f;
+              sc[h][t][i] = dp[h][t][i] * slope;
+            }
+          if (want_bias) {
+            float* bin = bins + (wave * p.copies + (p.copies > 1 ? t : 0)) * (a.B + 1) * kWave + lane;
+            add_to_bins(bin, b[0], dp[0][t]);
+            add_to_bins(bin, b[1], dp[1][t]);
           }
           sf[t] = as_operand<T>(sc[0][t], sc[1][t]);
         }
@@ -521,12 +547,13 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
         }
       }
     };
-    const int total = rtiles * grp;
-    if (total > 0) {
-      if (AHEAD) fetch(0);
-      if (BIAS) fetch_buckets(0);
+    const int all = rtiles * grp, per = (all + p.nsplit - 1) / p.nsplit;
+    const int first = min((int)blockIdx.y * per, all), total = min(first + per, all);
+    if (first < total) {
+      if (AHEAD) fetch(first);
+      if (BIAS) fetch_buckets(first);
     }
-    for (int it = 0; it < total; ++it) {
+    for (int it = first; it < total; ++it) {
       const int n = min(BR, s.nq - (it % rtiles) * BR);
       if (!AHEAD) fetch(it);
       __syncthreads();
@@ -617,6 +644,16 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
     for (int t = 0; t < KT; ++t) {
       if (key[t] < 0) continue;
       const int64_t at = ((int64_t)(s.k0 + key[t]) * a.Hk + kvh) * D;
+      if (p.nsplit > 1) {
+        const int64_t n = (int64_t)a.Nk * a.Hk * D;
+        float* to = p.part + 2 * blockIdx.y * n + at;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          store4<float>(to, d * 16 + g * 4, D, D % 4 == 0 ? 4 : 1, dk[t][d]);
+          store4<float>(to + n, d * 16 + g * 4, D, D % 4 == 0 && n % 4 == 0 ? 4 : 1, dv[t][d]);
+        }
+        continue;
+      }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         store4<T>(static_cast<T*>(p.dk) + at, d * 16 + g * 4, D, p.vec_dk, dk[t][d] * a.scale);
@@ -626,9 +663,27 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
   }
 }
 
-// Tiles of rows the first pass takes.
+// The parts of dk and dv added in order, an element a thread. Keys outside every graph
+// are left as they were.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void attn_grad_join(AttnGrad p) {
+  const AttnShape& a = p.a;
+  const int64_t n = (int64_t)a.Nk * a.Hk * a.D, i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  const int64_t w = (int64_t)a.Hk * a.D;
+  if (i >= n || i < a.koff[0] * w || i >= a.koff[a.G] * w) return;
+  float dk = 0.0f, dv = 0.0f;
+#pragma unroll 4
+  for (int sp = 0; sp < p.nsplit; ++sp) {
+    dk += p.part[2 * sp * n + i];
+    dv += p.part[(2 * sp + 1) * n + i];
+  }
+  static_cast<T*>(p.dk)[i] = to_type<T>(dk * a.scale);
+  static_cast<T*>(p.dv)[i] = to_type<T>(dv);
+}
+
+// Tiles of rows and keys that the two passes take.
 struct RowPlan {
-  int waves, qt, copies;
+  int waves, qt, copies, kt, nsplit;
   int64_t slots;
 };
 inline size_t bins_bytes(int waves, int copies, int64_t B) {
@@ -658,7 +713,7 @@ int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many key tiles");
   const size_t lds = bias_table_bytes(p.a);
   const bool cap = p.a.cap > 0.0f;
-  const unsigned n = (unsigned)blocks;
+  const dim3 n((unsigned)blocks, (unsigned)p.nsplit);
   if (p.a.B > 0) {
     if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, true, true><<<n, WAVES * kWave, lds, s>>>(p);
     else attn_grad_kv<T, DP, WAVES, KT, VEC, true, false><<<n, WAVES * kWave, lds, s>>>(p);
@@ -667,6 +722,11 @@ int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
     else attn_grad_kv<T, DP, WAVES, KT, VEC, false, false><<<n, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_grad_kv");
+  if (p.nsplit > 1) {
+    const int64_t values = (int64_t)p.a.Nk * p.a.Hk * p.a.D;
+    attn_grad_join<T><<<(unsigned)((values + kBlock - 1) / kBlock), kBlock, 0, s>>>(p);
+    TFG_LAUNCHED("attn_grad_join");
+  }
   return TFG_OK;
 }
 
@@ -693,7 +753,7 @@ int launch_grad_width(AttnGrad& p, const RowPlan& r, hipStream_t s) {
   }
   if (p.a.Nk == 0) return TFG_OK;
   if (!whole) return launch_grad_kv<T, DP, 4, 1, 0>(p, s);
-  if (DP * sizeof(T) < 512 && p.a.Nk / p.a.G > 192) return launch_grad_kv<T, DP, 4, 2, 8>(p, s);
+  if (r.kt == 2) return launch_grad_kv<T, DP, 4, 2, 8>(p, s);
   return launch_grad_kv<T, DP, 4, 1, 8>(p, s);
 }
 

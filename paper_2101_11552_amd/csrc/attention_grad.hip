@@ -7,25 +7,36 @@ namespace {
 
 constexpr size_t kMaxLds = 160 << 10;
 
-RowPlan row_plan(int64_t Nq, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B) {
-  const int64_t grp = H / Hk, rows = Nq * grp / std::max<int64_t>(G, 1);
-  RowPlan r{1, 1, 1, 0};
-  if (rows > 192) r = {4, 2, 1, 0};
-  else if (rows > 16) r = {4, 1, 1, 0};
+// Larger tiles where they still fill the card, which takes some kBlocks blocks: two row
+// (key) tiles a wavefront read each staged tile twice from LDS for four products. Heads
+// of more than 64 columns keep one: two take all registers of a SIMD for one wavefront.
+constexpr int64_t kBlocks = 768;
+
+RowPlan row_plan(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B) {
+  const int64_t grp = H / Hk, graphs = std::max<int64_t>(G, 1), rows = Nq * grp / graphs;
+  RowPlan r{1, 1, 1, 1, 1, 0};
+  if (rows > 192 && D <= 64 && rows / 128 * graphs * Hk >= kBlocks) r.waves = 4, r.qt = 2;
+  else if (rows > 16) r.waves = 4;
   if (16 % grp != 0) r.copies = r.qt;
   // the LDS of the tiles (three of 64 x DP bf16 or 32 x DP float32), the bias table and the bins
   const int64_t DP = D <= 16 ? 16 : D <= 32 ? 32 : D <= 64 ? 64 : 128;
   const size_t tiles = 3 * 2 * 64 * (size_t)(DP + 16) + 2 * 8 * (size_t)DP;
   if (tiles + sizeof(float) * (size_t)(grp * (B + 1)) + bins_bytes(r.waves, r.copies, B) > kMaxLds)
-    r = {1, 1, 1, 0};
+    r.waves = r.qt = r.copies = 1;
   r.slots = Nq * grp / (r.waves * r.qt * 16) + G;
+  const int64_t keys = Nk / graphs;
+  if (keys > 192 && D <= 64 && keys / 128 * graphs * Hk >= kBlocks) r.kt = 2;
+  // the queries of a key tile in parts of at least four tiles of rows
+  const int64_t blocks = std::max<int64_t>(keys / (64 * r.kt), 1) * graphs * Hk;
+  const int64_t tiles_of_rows = (Nq / graphs + 63) / 64 * grp;
+  r.nsplit = (int)std::max<int64_t>(std::min<int64_t>({kBlocks / blocks, tiles_of_rows / 4, 16}), 1);
   return r;
 }
 
 struct GradLayout {
-  size_t a, c, delta, part, sums, total;
+  size_t a, c, delta, part, sums, keys, total;
 };
-GradLayout grad_layout(int64_t Nq, int64_t H, int64_t B, const RowPlan& r) {
+GradLayout grad_layout(int64_t Nq, int64_t keys, int64_t H, int64_t B, const RowPlan& r) {
   GradLayout L;
   const size_t rows = align_up(sizeof(float) * (size_t)(Nq * H), 256);
   L.a = 0;
@@ -33,22 +44,23 @@ GradLayout grad_layout(int64_t Nq, int64_t H, int64_t B, const RowPlan& r) {
   L.delta = 2 * rows;
   L.part = 3 * rows;
   L.sums = L.part + align_up(sizeof(float) * (size_t)(B > 0 ? r.slots * H * B : 0), 256);
-  L.total = L.sums + align_up(B > 0 ? column_sums_bytes(r.slots, H * B) : 0, 256) + 256;
+  L.keys = L.sums + align_up(B > 0 ? column_sums_bytes(r.slots, H * B) : 0, 256);
+  L.total = L.keys + align_up(r.nsplit > 1 ? 2 * sizeof(float) * (size_t)(r.nsplit * keys) : 0, 256) + 256;
   return L;
 }
 
 }  // namespace
 
-size_t attention_backward_ws_bytes(int64_t Nq, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B) {
-  return grad_layout(Nq, H, B, row_plan(Nq, G, H, Hk, D, B)).total;
+size_t attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B) {
+  return grad_layout(Nq, Nk * Hk * D, H, B, row_plan(Nq, Nk, G, H, Hk, D, B)).total;
 }
 
 int launch_attention_backward(const AttnShape& a, int float_type, const void* q, const void* k,
                               const void* v, const void* out, const float* lse, const void* dout,
                               void* dq, void* dk, void* dv, void* dbias, void* ws, hipStream_t s) {
   if (a.G == 0 && dbias == nullptr) return TFG_OK;
-  const RowPlan r = row_plan(a.Nq, a.G, a.H, a.Hk, a.D, a.B);
-  const GradLayout L = grad_layout(a.Nq, a.H, a.B, r);
+  const RowPlan r = row_plan(a.Nq, a.Nk, a.G, a.H, a.Hk, a.D, a.B);
+  const GradLayout L = grad_layout(a.Nq, (int64_t)a.Nk * a.Hk * a.D, a.H, a.B, r);
   char* w = static_cast<char*>(ws);
   AttnGrad p{};
   p.a = a;
@@ -67,6 +79,8 @@ int launch_attention_backward(const AttnShape& a, int float_type, const void* q,
   p.row_delta = reinterpret_cast<float*>(w + L.delta);
   p.bias_part = dbias != nullptr ? reinterpret_cast<float*>(w + L.part) : nullptr;
   p.copies = r.copies;
+  p.nsplit = r.nsplit;
+  p.part = reinterpret_cast<float*>(w + L.keys);
   const bool narrow = a.D <= 32;
   int rc;
   if (float_type == TFG_BF16) rc = narrow ? launch_grad_bf16_narrow(p, r, s) : launch_grad_bf16_wide(p, r, s);

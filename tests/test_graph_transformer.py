@@ -466,6 +466,9 @@ SIZES = {
     "readout": [(1, 700), (1, 3), (1, 0), (1, 64)],
     "split": [(2, 3001), (2, 1500), (2, 1)],
     "many_queries": [(513, 33), (200, 1)],
+    # enough small graphs for a wavefront each, and a few larger ones among them
+    "many": [(64, 64), (65, 65), (0, 5), (5, 0), (1, 1), (64, 3), (3, 64), (200, 130), (16, 17), (33, 31)]
+            + [(7 * i % 61, 7 * i % 61) for i in range(70)] + [(i % 9, 60 - i) for i in range(48)],
 }
 
 
@@ -476,7 +479,9 @@ SIZES = {
     ("middle", 2, 2, 16, 20.0, 20), ("middle", 2, 1, 64, 0.0, 0), ("middle", 3, 1, 33, 5.0, 3),
     ("middle", 2, 1, 128, 50.0, 32), ("middle", 2, 2, 100, 0.0, 255),
     ("readout", 8, 2, 64, 0.0, 0), ("readout", 4, 4, 16, 2.0, 6), ("split", 16, 4, 64, 0.0, 0),
-    ("split", 2, 2, 48, 10.0, 12), ("many_queries", 4, 4, 80, 0.0, 7)])
+    ("split", 2, 2, 48, 10.0, 12), ("many_queries", 4, 4, 80, 0.0, 7),
+    ("many", 4, 4, 16, 0.0, 16), ("many", 8, 4, 8, 5.0, 0), ("many", 4, 4, 32, 80.0, 0),
+    ("many", 12, 4, 64, 3.0, 7), ("many", 4, 4, 128, 0.0, 0), ("many", 4, 4, 20, 0.0, 250)])
 def test_attention(tfg, name, sizes, H, Hk, D, cap, B):
     Case(name, SIZES[sizes], H, Hk, D, cap, B, seed=H * D + B).check(tfg)
 
@@ -485,9 +490,10 @@ def test_attention(tfg, name, sizes, H, Hk, D, cap, B):
 def test_attention_rows_outside_graphs(tfg, name):
     """Rows before the first graph and behind the last are left as they were."""
     import torch
-    for sizes in (SIZES["batch"], SIZES["split"], SIZES["middle"]):
-        c = Case(name, sizes, 2, 2, 24, 0.0, 4, seed=5, lead=3, trail=70)
-        out = torch.full((c.Nq, 48), 7.0, dtype=c.q.dtype, device="cuda")
+    for sizes in (SIZES["batch"], SIZES["split"], SIZES["middle"], SIZES["many"]):
+        heads = 4 if sizes is SIZES["many"] else 2
+        c = Case(name, sizes, heads, heads, 24, 0.0, 4, seed=5, lead=3, trail=70)
+        out = torch.full((c.Nq, heads * 24), 7.0, dtype=c.q.dtype, device="cuda")
         got, lse = c.forward(tfg, out=out)
         assert got is out
         assert bool((out[:3] == 7.0).all()) and bool((out[-70:] == 7.0).all())
