@@ -1165,7 +1165,9 @@ int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int
 
 size_t tfg_graph_attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t kv_heads,
                                     int64_t D) {
-  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1) return 0;
+  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1 ||
+      Nq >= kMaxCount || Nk >= kMaxCount || G >= kMaxCount || H > 1024 || D > max_attention_width())
+    return 0;
   return 256 + attention_ws_bytes(Nq, Nk, G, H, kv_heads, D);
 }
 
@@ -1193,8 +1195,11 @@ int tfg_graph_attention(const void *q, int64_t ldq, const void *k, int64_t ldk, 
 
 size_t tfg_graph_attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H,
                                              int64_t kv_heads, int64_t D, int64_t B) {
-  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1 || B < 0) return 0;
-  return 256 + attention_backward_ws_bytes(Nq, Nk, G, H, kv_heads, D, B);
+  if (Nq < 0 || Nk < 0 || G < 0 || H < 1 || kv_heads < 1 || H % kv_heads != 0 || D < 1 || B < 0 ||
+      Nq >= kMaxCount || Nk >= kMaxCount || G >= kMaxCount || H > 1024 || D > max_attention_width() || B > 255)
+    return 0;
+  return 256 + std::max(attention_backward_ws_bytes(TFG_F32, Nq, Nk, G, H, kv_heads, D, B),
+                        attention_backward_ws_bytes(TFG_BF16, Nq, Nk, G, H, kv_heads, D, B));
 }
 
 int tfg_graph_attention_backward(const void *dout, const void *q, int64_t ldq, const void *k,

@@ -685,6 +685,8 @@ __global__ __launch_bounds__(kBlock) void attn_grad_join(AttnGrad p) {
 struct RowPlan {
   int waves, qt, copies, kt, nsplit;
   int64_t slots;
+  int small_waves, small_block;  // of the launch over small graphs (0: none)
+  size_t small_lds;              // a wavefront's
 };
 inline size_t bins_bytes(int waves, int copies, int64_t B) {
   return sizeof(float) * (size_t)waves * copies * (B + 1) * kWave;
@@ -729,47 +731,5 @@ int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
   }
   return TFG_OK;
 }
-
-template <typename T, int DP>
-int launch_grad_width(AttnGrad& p, const RowPlan& r, hipStream_t s) {
-  const int D = p.a.D;
-  const int64_t ldo = (int64_t)p.a.H * D, ldk = (int64_t)p.a.Hk * D;
-  p.vec_q = row_vector<T>(p.q, p.a.ldq, D);
-  p.vec_k = row_vector<T>(p.k, p.a.ldk, D);
-  p.vec_v = row_vector<T>(p.v, p.a.ldv, D);
-  p.vec_o = row_vector<T>(p.out, ldo, D);
-  p.vec_do = row_vector<T>(p.dout, ldo, D);
-  p.vec_dq = row_vector<T>(p.dq, ldo, D);
-  p.vec_dk = row_vector<T>(p.dk, ldk, D);
-  p.vec_dv = row_vector<T>(p.dv, ldk, D);
-  p.heads = 1;
-  const bool whole = whole_vectors<T>(D);
-  if (p.a.Nq > 0) {
-    int rc;
-    if (r.qt == 2) rc = whole ? launch_grad_q<T, DP, 4, 2, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 2, 0>(p, r.slots, s);
-    else if (r.waves == 4) rc = whole ? launch_grad_q<T, DP, 4, 1, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 1, 0>(p, r.slots, s);
-    else rc = launch_grad_q<T, DP, 1, 1, 0>(p, r.slots, s);
-    if (rc) return rc;
-  }
-  if (p.a.Nk == 0) return TFG_OK;
-  if (!whole) return launch_grad_kv<T, DP, 4, 1, 0>(p, s);
-  if (r.kt == 2) return launch_grad_kv<T, DP, 4, 2, 8>(p, s);
-  return launch_grad_kv<T, DP, 4, 1, 8>(p, s);
-}
-
-// Heads of at most 32 columns, and wider ones (translation units of their own).
-template <typename T>
-int launch_grad_narrow(AttnGrad& p, const RowPlan& r, hipStream_t s) {
-  return p.a.D <= 16 ? launch_grad_width<T, 16>(p, r, s) : launch_grad_width<T, 32>(p, r, s);
-}
-template <typename T>
-int launch_grad_wide(AttnGrad& p, const RowPlan& r, hipStream_t s) {
-  return p.a.D <= 64 ? launch_grad_width<T, 64>(p, r, s) : launch_grad_width<T, 128>(p, r, s);
-}
-#define TFG_ATTN_GRAD(name) int launch_grad_##name(AttnGrad& p, const RowPlan& r, hipStream_t s)
-TFG_ATTN_GRAD(bf16_narrow);
-TFG_ATTN_GRAD(bf16_wide);
-TFG_ATTN_GRAD(f32_narrow);
-TFG_ATTN_GRAD(f32_wide);
 
 }  // namespace tfg

@@ -1,0 +1,365 @@
+// Gradients of the attention over many small graphs (gfx950): graphs of at most 64
+// queries and 64 keys, a wavefront for one (graph, key/value head) at a time, laid out as
+// attn_small. All five products of a graph in one pass:
+//   S = Q K^T, dP = dO V^T   with a key in each lane (l % 16), rows in its registers;
+//   dV^T += dO^T P, dK^T += Q^T dS   P and dS as they lie, dO and Q as columns in LDS;
+//   dQ^T = K^T dS^T          dS through LDS (rounded to the features' type), K as columns
+// A row's delta is summed from p and dp in float32 (all of its keys are here), and its
+// maximum and sum too where the log-sum has lost them (kLongLse). The bias bins stay in
+// LDS for all of a wavefront's graphs.
+#pragma once
+
+#include "attention_grad.h"
+#include "attention_small.h"
+
+namespace tfg {
+
+// Sum and maximum over the 16 lanes of a row of lanes, in all of them.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row16_sum(float x) {
+  x += dpp<0x128>(x);  // row_ror:8
+  x += dpp<0x124>(x);
+  x += dpp<0x122>(x);
+  x += dpp<0x121>(x);
+  return x;
+}
+__device__ __forceinline__ float row16_max(float x) {
+  x = fmaxf(x, dpp<0x128>(x));
+  x = fmaxf(x, dpp<0x124>(x));
+  x = fmaxf(x, dpp<0x122>(x));
+  x = fmaxf(x, dpp<0x121>(x));
+  return x;
+}
+
+// LDS of a wavefront: Q and dO of 32 rows as columns, K as columns, dS of 32 rows.
+template <typename T, int DP> struct SmallGrad {
+  static constexpr int LDR = 32 + lds_pad<T>(), LDK = kSmallGraph + lds_pad<T>();
+  static constexpr int elements = 2 * DP * LDR + DP * LDK + 32 * LDK;
+};
+inline int small_table(const AttnShape& a) {  // floats, a multiple of 16 bytes
+  return a.B > 0 ? (int)((bias_table_bytes(a) / 4 + 3) / 4 * 4) : 0;
+}
+inline int small_bins(const AttnShape& a, bool want) {
+  return want ? a.H / a.Hk * (a.B + 1) * kWave : 0;
+}
+
+template <typename T, int DP, bool BIAS, bool CAP>
+__global__ __launch_bounds__(4 * kWave) void attn_grad_small(AttnGrad p, int waves) {
+  using L = SmallGrad<T, DP>;
+  constexpr int LDR = L::LDR, LDK = L::LDK, KC = Frag<T, DP>::KC, DT = DP / 16, KT = kSmallTiles;
+  constexpr int KU = (kSmallGraph / 4 * (DP / 8) + kWave - 1) / kWave;
+  constexpr int RU = (8 * (DP / 8) + kWave - 1) / kWave;
+  extern __shared__ float dyn[];
+  const AttnShape& a = p.a;
+  const int grp = a.H / a.Hk, D = a.D;
+  const int wave = uniform((int)threadIdx.x / kWave), nw = (int)blockDim.x / kWave;
+  const int wid = (int)blockIdx.x * nw + wave;
+  if (wid >= waves) return;
+  const bool want_bias = BIAS && p.bias_part != nullptr;
+  const int tabn = BIAS ? (grp * (a.B + 1) + 3) & ~3 : 0, binn = want_bias ? grp * (a.B + 1) * kWave : 0;
+  float* tab = dyn + wave * (tabn + binn + L::elements * (int)sizeof(T) / 4);
+  float* bins = tab + tabn;
+  T* Qt = reinterpret_cast<T*>(bins + binn);
+  T* Ot = Qt + DP * LDR;
+  T* Kt = Ot + DP * LDR;
+  T* Ds = Kt + DP * LDK;
+  const int kvh = wid % a.Hk, lane = lane_id(), col = lane & 15, g = lane >> 4;
+  const ScoreScale sx = score_scale<T, BIAS, CAP>(a);
+  if (BIAS) load_bias<T>(a, kvh, grp, sx.add, tab, kWave, lane);
+  for (int i = lane; i < binn; i += kWave) bins[i] = 0.0f;
+  const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+
+  for (int gi = wid / a.Hk; gi < a.G; gi += waves / a.Hk) {
+    const Span s = small_span(a, uniform(gi));
+    if (s.g < 0) continue;
+    const uint8_t* dist = BIAS && s.nk > 0 ? dist_block(a, s) : nullptr;
+    const int kts = (s.nk + 15) / 16, last = s.nk - 1;
+    const T* kp = static_cast<const T*>(p.k) + (int64_t)s.k0 * a.ldk + (int64_t)kvh * D;
+    const T* vp = static_cast<const T*>(p.v) + (int64_t)s.k0 * a.ldv + (int64_t)kvh * D;
+    frag_t<T, DP> kf[KT][KC], vf[KT][KC];
+    f32x4 dk[KT][DT], dv[KT][DT];
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) dk[x][d] = dv[x][d] = zero;
+    if (s.nk > 0) {
+      x8_t<T> kr[KU][4];
+#pragma unroll
+      for (int x = 0; x < KT; ++x)
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+          const unsigned r = min(x * 16 + col, last);
+          kf[x][c] = frag_within<T, DP, true>(kp + r * (unsigned)a.ldk, c, g, D);
+          vf[x][c] = frag_within<T, DP, true>(vp + r * (unsigned)a.ldv, c, g, D);
+        }
+      using U = Units<kSmallGraph, DP>;
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {
+        const int c = u * kWave + lane;
+        if (U::quad_col(c) >= DP) continue;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          kr[u][i] = load8_within<T, 8>(kp, min(U::quad(c) * 4 + i, last) * (unsigned)a.ldk, U::quad_col(c), D);
+      }
+      wave_sync();
+#pragma unroll
+      for (int u = 0; u < KU; ++u) {  // K as columns, keys in their own order
+        const int c = u * kWave + lane, d0 = U::quad_col(c);
+        if (d0 >= DP) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          x4_t<T> w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = kr[u][i][e];
+          *reinterpret_cast<x4_t<T>*>(Kt + (d0 + e) * LDK + U::quad(c) * 4) = w;
+        }
+      }
+    }
+    for (int h = 0; h < grp; ++h) {
+      const int head = kvh * grp + h;
+      const float* th = tab + h * (a.B + 1);
+      for (int r0 = 0; r0 < s.nq; r0 += 32) {
+        const int n = min(32, s.nq - r0);
+        const int64_t node0 = s.q0 + r0;
+        const T* qp = static_cast<const T*>(p.q) + node0 * a.ldq + (int64_t)head * D;
+        const unsigned ldo = (unsigned)a.H * D;
+        const T* op = static_cast<const T*>(p.dout) + node0 * ldo + (int64_t)head * D;
+        // rows as operands, and as columns in LDS
+        frag_t<T, DP> qf[2][KC], of[2][KC];
+        unsigned bk[2][KT];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const unsigned r = min(x * 16 + col, n - 1);
+#pragma unroll
+          for (int c = 0; c < KC; ++c) {
+            qf[x][c] = frag_within<T, DP, false>(qp + r * (unsigned)a.ldq, c, g, D);
+            of[x][c] = frag_within<T, DP, false>(op + r * ldo, c, g, D);
+          }
+          if (BIAS) {
+            const int br = x * 16 + g * 4 + (col & 3);
+#pragma unroll
+            for (int y = 0; y < KT; ++y) {
+              bk[x][y] = 0xFFFFFFFFu;
+              if (dist != nullptr && br < n && y * 16 + (col & 12) < s.nk)
+                bk[x][y] = load_buckets(dist + (r0 + br) * s.nk, y * 16 + (col & 12), s.nk);
+            }
+          }
+        }
+        const float lse = p.lse[(node0 + min(lane & 31, n - 1)) * a.H + head];
+        x8_t<T> qr[RU][4], dr[RU][4];
+        using R = Units<32, DP>;
+#pragma unroll
+        for (int u = 0; u < RU; ++u) {
+          const int c = u * kWave + lane;
+          if (R::quad_col(c) >= DP) continue;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const unsigned r = min(R::quad(c) * 4 + i, n - 1);
+            qr[u][i] = load8_within<T, 8>(qp, r * (unsigned)a.ldq, R::quad_col(c), D);
+            dr[u][i] = load8_within<T, 8>(op, r * ldo, R::quad_col(c), D);
+          }
+        }
+        wave_sync();
+#pragma unroll
+        for (int u = 0; u < RU; ++u) {
+          const int c = u * kWave + lane;
+          if (R::quad_col(c) >= DP) continue;
+          put_columns<T, LDR>(Qt, R::quad(c), R::quad_col(c), qr[u]);
+          put_columns<T, LDR>(Ot, R::quad(c), R::quad_col(c), dr[u]);
+        }
+        const bool again = BIAS && __ballot(lse != -INFINITY && fabsf(lse) > kLongLse) != 0;
+        // p and dp of both row tiles
+        f32x4 sc[2][KT], dp[2][KT];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float ra[4], rc[4], delta[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = x * 16 + g * 4 + i;
+            const float ls = __shfl(lse, r);
+            ra[i] = r < n && ls != -INFINITY ? (BIAS ? ls : ls * kLog2e) : INFINITY;  // +inf: p = 0
+            rc[i] = delta[i] = 0.0f;
+          }
+          if (x * 16 >= n) {
+#pragma unroll
+            for (int y = 0; y < KT; ++y) sc[x][y] = dp[x][y] = zero;
+            continue;
+          }
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            sc[x][y] = dp[x][y] = zero;
+            if (y >= kts) continue;
+#pragma unroll
+            for (int c = 0; c < KC; ++c) {
+              sc[x][y] = mma(qf[x][c], kf[y][c], sc[x][y]);
+              dp[x][y] = mma(of[x][c], vf[y][c], dp[x][y]);
+            }
+            if (BIAS) bk[x][y] = transpose_quad(bk[x][y], (unsigned)(col & 3));
+          }
+          if (again) {
+            float m[4], l[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              m[i] = -INFINITY;
+              l[i] = 0.0f;
+#pragma unroll
+              for (int y = 0; y < KT; ++y)
+                if (y < kts) {
+                  const float add = th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
+                  m[i] = fmaxf(m[i], add == -INFINITY ? add : score<T, BIAS, CAP>(sc[x][y][i], add, sx));
+                }
+              m[i] = row16_max(m[i]);
+#pragma unroll
+              for (int y = 0; y < KT; ++y)
+                if (y < kts) {
+                  const float add = th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
+                  const float u = score<T, BIAS, CAP>(sc[x][y][i], add, sx);
+                  l[i] += add == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((u - m[i]) * kLog2e);
+                }
+              l[i] = row16_sum(l[i]);
+              if (l[i] != 0.0f) {
+                ra[i] = m[i];
+                rc[i] = -log2f(l[i]);
+              }
+            }
+          }
+          f32x4 slope[KT];
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            if (y >= kts) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float add = BIAS ? th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)] : sx.add;
+              const bool live = BIAS ? add != -INFINITY : y * 16 + col < s.nk;
+              const float e = weight<BIAS>(score<T, BIAS, CAP>(sc[x][y][i], add, sx), sx.unit, ra[i], rc[i]);
+              slope[y][i] = cap_slope<T, CAP>(sc[x][y][i], sx);
+              sc[x][y][i] = live ? e : 0.0f;
+              dp[x][y][i] = live ? dp[x][y][i] : 0.0f;
+              delta[i] = __builtin_fmaf(sc[x][y][i], dp[x][y][i], delta[i]);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) delta[i] = row16_sum(delta[i]);
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            if (y >= kts) continue;
+            unsigned b[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              dp[x][y][i] = sc[x][y][i] * (dp[x][y][i] - delta[i]);
+              b[i] = BIAS ? min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
+            }
+            if (want_bias) add_to_bins(bins + h * (a.B + 1) * kWave + lane, b, dp[x][y]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              if (CAP) dp[x][y][i] *= slope[y][i];
+              Ds[(x * 16 + g * 4 + i) * LDK + y * 16 + col] = to_type<T>(dp[x][y][i]);
+            }
+          }
+        }
+        wave_sync();
+        // dV, dK over these rows
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const x8_t<T> oc = lds8<T>(Ot + (d * 16 + col) * LDR + g * 8);
+          const x8_t<T> qc = lds8<T>(Qt + (d * 16 + col) * LDR + g * 8);
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            if (y >= kts) continue;
+            dv[y][d] = mma(oc, as_operand<T>(sc[0][y], sc[1][y]), dv[y][d]);
+            dk[y][d] = mma(qc, as_operand<T>(dp[0][y], dp[1][y]), dk[y][d]);
+          }
+        }
+        // dQ of these rows: dS has keys up to the next multiple of 32 (the last 16 may be
+        // another graph's: K's columns there are finite, dS's cleared)
+        if (kts & 1) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) Ds[(x * 16 + g * 4 + i) * LDK + kts * 16 + col] = (T)0.0f;
+          wave_sync();
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x * 16 >= n) break;
+          f32x4 o[DT];
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] = zero;
+#pragma unroll
+          for (int y = 0; y < KT / 2; ++y) {
+            if (2 * y >= kts) break;
+            const x8_t<T> sf = lds8<T>(Ds + (x * 16 + col) * LDK + y * 32 + g * 8);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = mma(lds8<T>(Kt + (d * 16 + col) * LDK + y * 32 + g * 8), sf, o[d]);
+          }
+          const int r = x * 16 + col;
+          if (r >= n) continue;
+          T* row = static_cast<T*>(p.dq) + ((node0 + r) * a.H + head) * D;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) store4<T>(row, d * 16 + g * 4, D, p.vec_dq, o[d] * a.scale);
+        }
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < KT; ++y) {
+      const int key = y * 16 + col;
+      if (key >= s.nk) continue;
+      const int64_t at = ((int64_t)(s.k0 + key) * a.Hk + kvh) * D;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        store4<T>(static_cast<T*>(p.dk) + at, d * 16 + g * 4, D, p.vec_dk, dk[y][d] * a.scale);
+        store4<T>(static_cast<T*>(p.dv) + at, d * 16 + g * 4, D, p.vec_dv, dv[y][d]);
+      }
+    }
+  }
+  if (!want_bias) return;
+  wave_sync();
+  for (int i = 0; i < grp * a.B; ++i) {
+    float sum = bins[(i / a.B * (a.B + 1) + i % a.B) * kWave + lane];
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) sum += __shfl_xor(sum, o);
+    if (lane == 0) p.bias_part[((int64_t)(wid / a.Hk) * a.H + (int64_t)kvh * grp) * a.B + i] = sum;
+  }
+}
+
+// The launch: wavefronts a block by what their LDS allows, wavefronts in all by how many
+// blocks the card holds at once; 0: the kernel does not take this shape.
+struct SmallPlan {
+  int waves, per_block;
+  size_t lds;  // a wavefront
+};
+inline SmallPlan small_grad_plan(int float_type, const AttnShape& a, bool want) {
+  SmallPlan r{0, 0, 0};
+  const size_t sz = float_type == TFG_BF16 ? 2 : 4;
+  const int DP = a.D <= 16 ? 16 : a.D <= 32 ? 32 : 64, per = (int)(16 / sz);
+  if (a.D > 64 || (sz == 4 && a.D > 32) || a.D % per != 0 || !small_graphs(a.Nq, a.Nk, a.G, a.Hk)) return r;
+  const size_t elements = 2 * DP * (32 + per) + DP * (kSmallGraph + per) + 32 * (kSmallGraph + per);
+  r.lds = sizeof(float) * (size_t)(small_table(a) + small_bins(a, want)) + sz * elements;
+  if (r.lds > (40u << 10)) return r;
+  r.per_block = 4;
+  const int blocks = (int)std::min<size_t>((160u << 10) / (4 * r.lds), 2);  // a CU (two wavefronts a SIMD)
+  r.waves = small_waves(a, 4 * blocks * 2);  // two rounds of them
+  return r;
+}
+
+template <typename T, int DP>
+int launch_grad_small(const AttnGrad& p, const SmallPlan& r, hipStream_t s) {
+  const unsigned blocks = (unsigned)((r.waves + r.per_block - 1) / r.per_block);
+  const unsigned threads = r.per_block * kWave;
+  const size_t lds = r.lds * r.per_block;
+  const bool cap = p.a.cap > 0.0f;
+  if (p.a.B > 0) {
+    if (cap) attn_grad_small<T, DP, true, true><<<blocks, threads, lds, s>>>(p, r.waves);
+    else attn_grad_small<T, DP, true, false><<<blocks, threads, lds, s>>>(p, r.waves);
+  } else {
+    if (cap) attn_grad_small<T, DP, false, true><<<blocks, threads, lds, s>>>(p, r.waves);
+    else attn_grad_small<T, DP, false, false><<<blocks, threads, lds, s>>>(p, r.waves);
+  }
+  TFG_LAUNCHED("attn_grad_small");
+  return TFG_OK;
+}
+
+}  // namespace tfg

@@ -277,7 +277,8 @@ int max_attention_bias_entries();  // (H / Hk) * B
 size_t attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk, int64_t D);
 int launch_attention(const AttnShape& a, int float_type, const void* q, const void* k,
                      const void* v, void* out, float* lse, void* ws, hipStream_t s);
-size_t attention_backward_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk, int64_t D, int64_t B);
+size_t attention_backward_ws_bytes(int float_type, int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk,
+                                   int64_t D, int64_t B);
 int launch_attention_backward(const AttnShape& a, int float_type, const void* q, const void* k,
                               const void* v, const void* out, const float* lse, const void* dout,
                               void* dq, void* dk, void* dv, void* dbias, void* ws, hipStream_t s);
