@@ -34,11 +34,25 @@ __device__ __forceinline__ float row16_max(float x) {
   return x;
 }
 
-// LDS of a wavefront: Q and dO of 32 rows as columns, K as columns, dS of 32 rows.
+template <typename T>
+__device__ __forceinline__ x8_t<T> join4(x4_t<T> a, x4_t<T> b) {
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// LDS of a wavefront: Q and dO of 16 rows as columns, K as columns, dS of 16 rows.
 template <typename T, int DP> struct SmallGrad {
-  static constexpr int LDR = 32 + lds_pad<T>(), LDK = kSmallGraph + lds_pad<T>();
-  static constexpr int elements = 2 * DP * LDR + DP * LDK + 32 * LDK;
+  static constexpr int LDR = 16 + lds_pad<T>(), LDK = kSmallGraph + lds_pad<T>();
+  static constexpr int elements = 2 * DP * LDR + DP * LDK + 16 * LDK;
 };
+// A lane's chunks of row (or key) `at` as columns.
+template <typename T, int DP, int LD>
+__device__ __forceinline__ void put_frag_columns(T* dst, int at, int g, const frag_t<T, DP> (&v)[Frag<T, DP>::KC]) {
+#pragma unroll
+  for (int c = 0; c < Frag<T, DP>::KC; ++c)
+#pragma unroll
+    for (int e = 0; e < Frag<T, DP>::N; ++e)
+      dst[(c * Frag<T, DP>::W + g * Frag<T, DP>::N + e) * LD + at] = v[c][e];
+}
 inline int small_table(const AttnShape& a) {  // floats, a multiple of 16 bytes
   return a.B > 0 ? (int)((bias_table_bytes(a) / 4 + 3) / 4 * 4) : 0;
 }
@@ -50,8 +64,6 @@ template <typename T, int DP, bool BIAS, bool CAP>
 __global__ __launch_bounds__(4 * kWave) void attn_grad_small(AttnGrad p, int waves) {
   using L = SmallGrad<T, DP>;
   constexpr int LDR = L::LDR, LDK = L::LDK, KC = Frag<T, DP>::KC, DT = DP / 16, KT = kSmallTiles;
-  constexpr int KU = (kSmallGraph / 4 * (DP / 8) + kWave - 1) / kWave;
-  constexpr int RU = (8 * (DP / 8) + kWave - 1) / kWave;
   extern __shared__ float dyn[];
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
@@ -77,8 +89,6 @@ __global__ __launch_bounds__(4 * kWave) void attn_grad_small(AttnGrad p, int wav
     if (s.g < 0) continue;
     const uint8_t* dist = BIAS && s.nk > 0 ? dist_block(a, s) : nullptr;
     const int kts = (s.nk + 15) / 16, last = s.nk - 1;
-    const T* kp = static_cast<const T*>(p.k) + (int64_t)s.k0 * a.ldk + (int64_t)kvh * D;
-    const T* vp = static_cast<const T*>(p.v) + (int64_t)s.k0 * a.ldv + (int64_t)kvh * D;
     frag_t<T, DP> kf[KT][KC], vf[KT][KC];
     f32x4 dk[KT][DT], dv[KT][DT];
 #pragma unroll
@@ -86,7 +96,8 @@ __global__ __launch_bounds__(4 * kWave) void attn_grad_small(AttnGrad p, int wav
 #pragma unroll
       for (int d = 0; d < DT; ++d) dk[x][d] = dv[x][d] = zero;
     if (s.nk > 0) {
-      x8_t<T> kr[KU][4];
+      const T* kp = static_cast<const T*>(p.k) + (int64_t)s.k0 * a.ldk + (int64_t)kvh * D;
+      const T* vp = static_cast<const T*>(p.v) + (int64_t)s.k0 * a.ldv + (int64_t)kvh * D;
 #pragma unroll
       for (int x = 0; x < KT; ++x)
 #pragma unroll
@@ -95,209 +106,149 @@ __global__ __launch_bounds__(4 * kWave) void attn_grad_small(AttnGrad p, int wav
           kf[x][c] = frag_within<T, DP, true>(kp + r * (unsigned)a.ldk, c, g, D);
           vf[x][c] = frag_within<T, DP, true>(vp + r * (unsigned)a.ldv, c, g, D);
         }
-      using U = Units<kSmallGraph, DP>;
-#pragma unroll
-      for (int u = 0; u < KU; ++u) {
-        const int c = u * kWave + lane;
-        if (U::quad_col(c) >= DP) continue;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          kr[u][i] = load8_within<T, 8>(kp, min(U::quad(c) * 4 + i, last) * (unsigned)a.ldk, U::quad_col(c), D);
-      }
       wave_sync();
 #pragma unroll
-      for (int u = 0; u < KU; ++u) {  // K as columns, keys in their own order
-        const int c = u * kWave + lane, d0 = U::quad_col(c);
-        if (d0 >= DP) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          x4_t<T> w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = kr[u][i][e];
-          *reinterpret_cast<x4_t<T>*>(Kt + (d0 + e) * LDK + U::quad(c) * 4) = w;
-        }
-      }
+      for (int x = 0; x < KT; ++x) put_frag_columns<T, DP, LDK>(Kt, x * 16 + col, g, kf[x]);
     }
     for (int h = 0; h < grp; ++h) {
       const int head = kvh * grp + h;
       const float* th = tab + h * (a.B + 1);
-      for (int r0 = 0; r0 < s.nq; r0 += 32) {
-        const int n = min(32, s.nq - r0);
+      for (int r0 = 0; r0 < s.nq; r0 += 16) {
+        const int n = min(16, s.nq - r0);
         const int64_t node0 = s.q0 + r0;
-        const T* qp = static_cast<const T*>(p.q) + node0 * a.ldq + (int64_t)head * D;
-        const unsigned ldo = (unsigned)a.H * D;
-        const T* op = static_cast<const T*>(p.dout) + node0 * ldo + (int64_t)head * D;
+        const unsigned r = min(col, n - 1);
         // rows as operands, and as columns in LDS
-        frag_t<T, DP> qf[2][KC], of[2][KC];
-        unsigned bk[2][KT];
+        frag_t<T, DP> qf[KC], of[KC];
+        unsigned bk[KT];
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const unsigned r = min(x * 16 + col, n - 1);
+        for (int c = 0; c < KC; ++c) {
+          qf[c] = frag_within<T, DP, false>(static_cast<const T*>(p.q) + (node0 + r) * a.ldq + (int64_t)head * D, c, g, D);
+          of[c] = frag_within<T, DP, false>(static_cast<const T*>(p.dout) + ((node0 + r) * a.H + head) * D, c, g, D);
+        }
+        if (BIAS) {
+          const int br = g * 4 + (col & 3);
+#pragma unroll
+          for (int y = 0; y < KT; ++y) {
+            bk[y] = 0xFFFFFFFFu;
+            if (dist != nullptr && br < n && y * 16 + (col & 12) < s.nk)
+              bk[y] = load_buckets(dist + (r0 + br) * s.nk, y * 16 + (col & 12), s.nk);
+          }
+        }
+        const float lse = p.lse[(node0 + r) * a.H + head];
+        wave_sync();
+        put_frag_columns<T, DP, LDR>(Qt, col, g, qf);
+        put_frag_columns<T, DP, LDR>(Ot, col, g, of);
+        const bool again = BIAS && __ballot(lse != -INFINITY && fabsf(lse) > kLongLse) != 0;
+        float ra[4], rc[4], delta[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ls = __shfl(lse, g * 4 + i);
+          ra[i] = g * 4 + i < n && ls != -INFINITY ? (BIAS ? ls : ls * kLog2e) : INFINITY;  // +inf: p = 0
+          rc[i] = delta[i] = 0.0f;
+        }
+        f32x4 sc[KT], dp[KT];
+#pragma unroll
+        for (int y = 0; y < KT; ++y) {
+          if (y >= kts) break;
+          sc[y] = dp[y] = zero;
 #pragma unroll
           for (int c = 0; c < KC; ++c) {
-            qf[x][c] = frag_within<T, DP, false>(qp + r * (unsigned)a.ldq, c, g, D);
-            of[x][c] = frag_within<T, DP, false>(op + r * ldo, c, g, D);
+            sc[y] = mma(qf[c], kf[y][c], sc[y]);
+            dp[y] = mma(of[c], vf[y][c], dp[y]);
           }
-          if (BIAS) {
-            const int br = x * 16 + g * 4 + (col & 3);
-#pragma unroll
-            for (int y = 0; y < KT; ++y) {
-              bk[x][y] = 0xFFFFFFFFu;
-              if (dist != nullptr && br < n && y * 16 + (col & 12) < s.nk)
-                bk[x][y] = load_buckets(dist + (r0 + br) * s.nk, y * 16 + (col & 12), s.nk);
-            }
-          }
+          if (BIAS) bk[y] = transpose_quad(bk[y], (unsigned)(col & 3));
         }
-        const float lse = p.lse[(node0 + min(lane & 31, n - 1)) * a.H + head];
-        x8_t<T> qr[RU][4], dr[RU][4];
-        using R = Units<32, DP>;
-#pragma unroll
-        for (int u = 0; u < RU; ++u) {
-          const int c = u * kWave + lane;
-          if (R::quad_col(c) >= DP) continue;
+        if (again) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const unsigned r = min(R::quad(c) * 4 + i, n - 1);
-            qr[u][i] = load8_within<T, 8>(qp, r * (unsigned)a.ldq, R::quad_col(c), D);
-            dr[u][i] = load8_within<T, 8>(op, r * ldo, R::quad_col(c), D);
-          }
-        }
-        wave_sync();
+            float m = -INFINITY, l = 0.0f;
 #pragma unroll
-        for (int u = 0; u < RU; ++u) {
-          const int c = u * kWave + lane;
-          if (R::quad_col(c) >= DP) continue;
-          put_columns<T, LDR>(Qt, R::quad(c), R::quad_col(c), qr[u]);
-          put_columns<T, LDR>(Ot, R::quad(c), R::quad_col(c), dr[u]);
-        }
-        const bool again = BIAS && __ballot(lse != -INFINITY && fabsf(lse) > kLongLse) != 0;
-        // p and dp of both row tiles
-        f32x4 sc[2][KT], dp[2][KT];
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float ra[4], rc[4], delta[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = x * 16 + g * 4 + i;
-            const float ls = __shfl(lse, r);
-            ra[i] = r < n && ls != -INFINITY ? (BIAS ? ls : ls * kLog2e) : INFINITY;  // +inf: p = 0
-            rc[i] = delta[i] = 0.0f;
-          }
-          if (x * 16 >= n) {
-#pragma unroll
-            for (int y = 0; y < KT; ++y) sc[x][y] = dp[x][y] = zero;
-            continue;
-          }
-#pragma unroll
-          for (int y = 0; y < KT; ++y) {
-            sc[x][y] = dp[x][y] = zero;
-            if (y >= kts) continue;
-#pragma unroll
-            for (int c = 0; c < KC; ++c) {
-              sc[x][y] = mma(qf[x][c], kf[y][c], sc[x][y]);
-              dp[x][y] = mma(of[x][c], vf[y][c], dp[x][y]);
-            }
-            if (BIAS) bk[x][y] = transpose_quad(bk[x][y], (unsigned)(col & 3));
-          }
-          if (again) {
-            float m[4], l[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              m[i] = -INFINITY;
-              l[i] = 0.0f;
-#pragma unroll
-              for (int y = 0; y < KT; ++y)
-                if (y < kts) {
-                  const float add = th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
-                  m[i] = fmaxf(m[i], add == -INFINITY ? add : score<T, BIAS, CAP>(sc[x][y][i], add, sx));
-                }
-              m[i] = row16_max(m[i]);
-#pragma unroll
-              for (int y = 0; y < KT; ++y)
-                if (y < kts) {
-                  const float add = th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
-                  const float u = score<T, BIAS, CAP>(sc[x][y][i], add, sx);
-                  l[i] += add == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((u - m[i]) * kLog2e);
-                }
-              l[i] = row16_sum(l[i]);
-              if (l[i] != 0.0f) {
-                ra[i] = m[i];
-                rc[i] = -log2f(l[i]);
+            for (int y = 0; y < KT; ++y)
+              if (y < kts) {
+                const float add = th[min((bk[y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
+                m = fmaxf(m, add == -INFINITY ? add : score<T, BIAS, CAP>(sc[y][i], add, sx));
               }
+            m = row16_max(m);
+#pragma unroll
+            for (int y = 0; y < KT; ++y)
+              if (y < kts) {
+                const float add = th[min((bk[y] >> (8 * i)) & 0xFFu, (unsigned)a.B)];
+                const float u = score<T, BIAS, CAP>(sc[y][i], add, sx);
+                l += add == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((u - m) * kLog2e);
+              }
+            l = row16_sum(l);
+            if (l != 0.0f) {
+              ra[i] = m;
+              rc[i] = -log2f(l);
             }
           }
-          f32x4 slope[KT];
+        }
+        f32x4 slope[KT];
 #pragma unroll
-          for (int y = 0; y < KT; ++y) {
-            if (y >= kts) continue;
+        for (int y = 0; y < KT; ++y) {
+          if (y >= kts) break;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float add = BIAS ? th[min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B)] : sx.add;
-              const bool live = BIAS ? add != -INFINITY : y * 16 + col < s.nk;
-              const float e = weight<BIAS>(score<T, BIAS, CAP>(sc[x][y][i], add, sx), sx.unit, ra[i], rc[i]);
-              slope[y][i] = cap_slope<T, CAP>(sc[x][y][i], sx);
-              sc[x][y][i] = live ? e : 0.0f;
-              dp[x][y][i] = live ? dp[x][y][i] : 0.0f;
-              delta[i] = __builtin_fmaf(sc[x][y][i], dp[x][y][i], delta[i]);
-            }
+          for (int i = 0; i < 4; ++i) {
+            const float add = BIAS ? th[min((bk[y] >> (8 * i)) & 0xFFu, (unsigned)a.B)] : sx.add;
+            const bool live = BIAS ? add != -INFINITY : y * 16 + col < s.nk;
+            const float e = weight<BIAS>(score<T, BIAS, CAP>(sc[y][i], add, sx), sx.unit, ra[i], rc[i]);
+            slope[y][i] = cap_slope<T, CAP>(sc[y][i], sx);
+            sc[y][i] = live ? e : 0.0f;
+            dp[y][i] = live ? dp[y][i] : 0.0f;
+            delta[i] = __builtin_fmaf(sc[y][i], dp[y][i], delta[i]);
           }
+        }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) delta[i] = row16_sum(delta[i]);
+        for (int i = 0; i < 4; ++i) delta[i] = row16_sum(delta[i]);
+        x4_t<T> pf[KT], sf[KT];
 #pragma unroll
-          for (int y = 0; y < KT; ++y) {
-            if (y >= kts) continue;
-            unsigned b[4];
+        for (int y = 0; y < KT; ++y) {
+          if (y >= kts) break;
+          unsigned b[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              dp[x][y][i] = sc[x][y][i] * (dp[x][y][i] - delta[i]);
-              b[i] = BIAS ? min((bk[x][y] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
-            }
-            if (want_bias) add_to_bins(bins + h * (a.B + 1) * kWave + lane, b, dp[x][y]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (CAP) dp[x][y][i] *= slope[y][i];
-              Ds[(x * 16 + g * 4 + i) * LDK + y * 16 + col] = to_type<T>(dp[x][y][i]);
-            }
+          for (int i = 0; i < 4; ++i) {
+            dp[y][i] = sc[y][i] * (dp[y][i] - delta[i]);
+            b[i] = BIAS ? min((bk[y] >> (8 * i)) & 0xFFu, (unsigned)a.B) : 0;
           }
+          if (want_bias) add_to_bins(bins + h * (a.B + 1) * kWave + lane, b, dp[y]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pf[y][i] = to_type<T>(sc[y][i]);
+            sf[y][i] = to_type<T>(CAP ? dp[y][i] * slope[y][i] : dp[y][i]);
+            Ds[(g * 4 + i) * LDK + y * 16 + col] = sf[y][i];
+          }
+        }
+        // the keys from kts * 16 to the next multiple of 32 have no weight
+        if (kts & 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) Ds[(g * 4 + i) * LDK + kts * 16 + col] = (T)0.0f;
         }
         wave_sync();
         // dV, dK over these rows
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const x8_t<T> oc = lds8<T>(Ot + (d * 16 + col) * LDR + g * 8);
-          const x8_t<T> qc = lds8<T>(Qt + (d * 16 + col) * LDR + g * 8);
+          const x4_t<T> oc = *reinterpret_cast<const x4_t<T>*>(Ot + (d * 16 + col) * LDR + g * 4);
+          const x4_t<T> qc = *reinterpret_cast<const x4_t<T>*>(Qt + (d * 16 + col) * LDR + g * 4);
 #pragma unroll
           for (int y = 0; y < KT; ++y) {
-            if (y >= kts) continue;
-            dv[y][d] = mma(oc, as_operand<T>(sc[0][y], sc[1][y]), dv[y][d]);
-            dk[y][d] = mma(qc, as_operand<T>(dp[0][y], dp[1][y]), dk[y][d]);
+            if (y >= kts) break;
+            dv[y][d] = mma(oc, pf[y], dv[y][d]);
+            dk[y][d] = mma(qc, sf[y], dk[y][d]);
           }
         }
-        // dQ of these rows: dS has keys up to the next multiple of 32 (the last 16 may be
-        // another graph's: K's columns there are finite, dS's cleared)
-        if (kts & 1) {
+        // dQ of these rows
+        f32x4 o[DT];
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+        for (int d = 0; d < DT; ++d) o[d] = zero;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) Ds[(x * 16 + g * 4 + i) * LDK + kts * 16 + col] = (T)0.0f;
-          wave_sync();
+        for (int y = 0; y < KT / 2; ++y) {
+          if (2 * y >= kts) break;
+          const x8_t<T> ds = lds8<T>(Ds + col * LDK + y * 32 + g * 8);
+#pragma unroll
+          for (int d = 0; d < DT; ++d) o[d] = mma(lds8<T>(Kt + (d * 16 + col) * LDK + y * 32 + g * 8), ds, o[d]);
         }
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (x * 16 >= n) break;
-          f32x4 o[DT];
-#pragma unroll
-          for (int d = 0; d < DT; ++d) o[d] = zero;
-#pragma unroll
-          for (int y = 0; y < KT / 2; ++y) {
-            if (2 * y >= kts) break;
-            const x8_t<T> sf = lds8<T>(Ds + (x * 16 + col) * LDK + y * 32 + g * 8);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = mma(lds8<T>(Kt + (d * 16 + col) * LDK + y * 32 + g * 8), sf, o[d]);
-          }
-          const int r = x * 16 + col;
-          if (r >= n) continue;
-          T* row = static_cast<T*>(p.dq) + ((node0 + r) * a.H + head) * D;
+        if (col < n) {
+          T* row = static_cast<T*>(p.dq) + ((node0 + col) * a.H + head) * D;
 #pragma unroll
           for (int d = 0; d < DT; ++d) store4<T>(row, d * 16 + g * 4, D, p.vec_dq, o[d] * a.scale);
         }
@@ -336,11 +287,11 @@ inline SmallPlan small_grad_plan(int float_type, const AttnShape& a, bool want) 
   const size_t sz = float_type == TFG_BF16 ? 2 : 4;
   const int DP = a.D <= 16 ? 16 : a.D <= 32 ? 32 : 64, per = (int)(16 / sz);
   if (a.D > 64 || (sz == 4 && a.D > 32) || a.D % per != 0 || !small_graphs(a.Nq, a.Nk, a.G, a.Hk)) return r;
-  const size_t elements = 2 * DP * (32 + per) + DP * (kSmallGraph + per) + 32 * (kSmallGraph + per);
+  const size_t elements = 2 * DP * (16 + per) + DP * (kSmallGraph + per) + 16 * (kSmallGraph + per);
   r.lds = sizeof(float) * (size_t)(small_table(a) + small_bins(a, want)) + sz * elements;
   if (r.lds > (40u << 10)) return r;
   r.per_block = 4;
-  const int blocks = (int)std::min<size_t>((160u << 10) / (4 * r.lds), 2);  // a CU (two wavefronts a SIMD)
+  const int blocks = (int)std::min<size_t>((160u << 10) / (4 * r.lds), 3);  // a CU
   r.waves = small_waves(a, 4 * blocks * 2);  // two rounds of them
   return r;
 }
