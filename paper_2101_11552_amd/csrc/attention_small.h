@@ -14,12 +14,6 @@ namespace tfg {
 constexpr int kSmallGraph = 64;
 constexpr int kSmallTiles = kSmallGraph / 16;
 
-// Orders a wavefront's LDS accesses (its lanes exchange values through LDS).
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // The graph's rows, or g < 0 where another launch has it.
 __device__ __forceinline__ Span small_span(const AttnShape& a, int g) {
   Span s;

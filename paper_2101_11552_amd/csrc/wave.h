@@ -10,6 +10,12 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 
 __device__ __forceinline__ int lane_id() { return threadIdx.x & (kWave - 1); }
 
+// Orders a wavefront's LDS accesses (its lanes exchange values through LDS).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Inclusive scan over the wavefront (all lanes active) with DPP moves: shifts
 // inside each row of 16 lanes, then the row totals carried to the rows after.
 __device__ __forceinline__ int wave_incl_scan(int v) {
