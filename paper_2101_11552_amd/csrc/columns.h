@@ -20,10 +20,12 @@ __global__ __launch_bounds__(kWave* kSumLanes) void column_sums(const In* __rest
   const int64_t r0 = blockIdx.y * per, r1 = min(r0 + per, rows);
   double acc[4] = {};
   if (c < n)
-    for (int64_t r = r0 + y; r < r1; r += 4 * kSumLanes) {
+    for (int64_t r = r0 + y; r < r1; r += 8 * kSumLanes) {
+      In x[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (r + u * kSumLanes < r1) acc[u] += (double)in[(r + u * kSumLanes) * n + c];
+      for (int u = 0; u < 8; ++u) x[u] = in[min(r + u * kSumLanes, r1 - 1) * n + c];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) acc[u % 4] += r + u * kSumLanes < r1 ? (double)x[u] : 0.0;
     }
   part[y][x] = (acc[0] + acc[1]) + (acc[2] + acc[3]);
   __syncthreads();

@@ -1,6 +1,8 @@
 // Rows of a table by id, and the table's gradient by sorted ids (gfx950).
 //
-// Forward: out[n] = scale * table[ids[n]], a row copy: bound by memory.
+// Forward: out[n] = scale * table[ids[n]], a row copy: bound by memory. A lane takes 16
+// bytes of a row of any width; where the width is no multiple of that, the row's last
+// lane steps back to end at its last column (and writes some again, the same).
 //
 // Gradient: dtable[v] = scale * sum of dout[n] over the n with ids[n] = v. The ids
 // are sorted (stable, csr.hip), so that every row's terms are a run of sorted
@@ -42,8 +44,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_rows(
     id[u] = off ? 0 : id[u] == pad ? -1 : id[u];  // (pad lies in the table, or is negative)
   }
   if (bad && err != nullptr && sub == 0 && blockIdx.y == 0) atomicOr(err, kErrIndex);
-  const int c = (blockIdx.y * lpr + sub) * V;
-  if (c >= F) return;
+  const int cw = (blockIdx.y * lpr + sub) * V, c = min(cw, F - V);
+  if (cw >= F) return;
   float x[kEmbRows][V];
 #pragma unroll
   for (int u = 0; u < kEmbRows; ++u) {
@@ -78,8 +80,8 @@ __global__ __launch_bounds__(kEmbThreads) void embed_grad_tiles(EmbedGrad p) {
   const int r = threadIdx.x / p.lpr, sub = threadIdx.x - r * p.lpr;
   const int64_t tile = (int64_t)blockIdx.x * p.rp + r;
   const int64_t b = tile * kEmbedTile;
-  const int c = (blockIdx.y * p.lpr + sub) * V;
-  if (r >= p.rp || b >= p.N || c >= p.F) return;
+  const int cw = (blockIdx.y * p.lpr + sub) * V, c = min(cw, p.F - V);
+  if (r >= p.rp || b >= p.N || cw >= p.F) return;
   const int64_t e = min(b + kEmbedTile, p.N);
   const T* dout = static_cast<const T*>(p.dout);
   T* dtable = static_cast<T*>(p.dtable);
@@ -102,17 +104,32 @@ __global__ __launch_bounds__(kEmbThreads) void embed_grad_tiles(EmbedGrad p) {
       for (int v = 0; v < V; ++v) to[v] = acc[v];
     }
   };
+  // the ids and places of the next rows are loaded while these are added
+  int kn[kEmbU], an[kEmbU];
+#pragma unroll
+  for (int u = 0; u < kEmbU; ++u) {
+    const int64_t n = min(b + u, e - 1);
+    kn[u] = p.key[n];
+    an[u] = p.perm[n];
+  }
   for (int64_t n0 = b; n0 < e; n0 += kEmbU) {
     int k[kEmbU], at[kEmbU];
     float x[kEmbU][V];
 #pragma unroll
     for (int u = 0; u < kEmbU; ++u) {
-      const int64_t n = min(n0 + u, e - 1);
-      k[u] = p.key[n];
-      at[u] = p.perm[n];
+      k[u] = kn[u];
+      at[u] = an[u];
     }
 #pragma unroll
     for (int u = 0; u < kEmbU; ++u) load_cols<T, V>(dout + (int64_t)at[u] * p.F + c, x[u]);
+    if (n0 + kEmbU < e) {
+#pragma unroll
+      for (int u = 0; u < kEmbU; ++u) {
+        const int64_t n = min(n0 + kEmbU + u, e - 1);
+        kn[u] = p.key[n];
+        an[u] = p.perm[n];
+      }
+    }
 #pragma unroll
     for (int u = 0; u < kEmbU; ++u)
       if (n0 + u < e) {
@@ -130,6 +147,21 @@ __global__ __launch_bounds__(kEmbThreads) void embed_grad_tiles(EmbedGrad p) {
   flush(after != cur);
 }
 
+// V floats at any address of one.
+template <int V>
+__device__ __forceinline__ void load_floats(const float* p, float (&x)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int h = 0; h < V; h += 4) {
+      const f32x4 t = *reinterpret_cast<const any4_t<float>*>(p + h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[h + i] = t[i];
+    }
+  } else {
+    x[0] = *p;
+  }
+}
+
 // Runs over several tiles: the block of the tile in which a run starts and that it
 // leaves adds tail[tile] and the heads of the tiles behind it, rp groups of lanes
 // each every rp-th head, joined in order.
@@ -144,20 +176,23 @@ __global__ __launch_bounds__(kEmbThreads) void embed_grad_join(EmbedGrad p) {
   if (b / kEmbedTile != tile) return;  // it starts in an earlier tile
   const int64_t last = (end - 1) / kEmbedTile;
   const int r = threadIdx.x / p.lpr, sub = threadIdx.x - r * p.lpr;
-  const int c = (blockIdx.y * p.lpr + sub) * V;
-  const bool on = r < p.rp && c < p.F;
+  const int cw = (blockIdx.y * p.lpr + sub) * V, c = min(cw, p.F - V);
+  const bool on = r < p.rp && cw < p.F;
   float acc[kJoinU][V];
 #pragma unroll
   for (int u = 0; u < kJoinU; ++u)
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[u][v] = 0.0f;
   if (on) {
-    for (int64_t t = tile + 1 + r; t <= last; t += kJoinU * p.rp)
+    for (int64_t t = tile + 1 + r; t <= last; t += kJoinU * p.rp) {
+      float x[kJoinU][V];
+#pragma unroll
+      for (int u = 0; u < kJoinU; ++u) load_floats<V>(p.head + min(t + u * p.rp, last) * p.F + c, x[u]);
 #pragma unroll
       for (int u = 0; u < kJoinU; ++u)
-        if (t + u * p.rp <= last)
 #pragma unroll
-          for (int v = 0; v < V; ++v) acc[u][v] += p.head[(t + u * p.rp) * p.F + c + v];
+        for (int v = 0; v < V; ++v) acc[u][v] += t + u * p.rp <= last ? x[u][v] : 0.0f;
+    }
 #pragma unroll
     for (int h = kJoinU / 2; h > 0; h >>= 1)
 #pragma unroll
@@ -184,8 +219,8 @@ template <typename T, int V>
 __global__ __launch_bounds__(kEmbThreads) void embed_grad_zero(EmbedGrad p) {
   const int r = threadIdx.x / p.lpr, sub = threadIdx.x - r * p.lpr;
   const int64_t v0 = ((int64_t)blockIdx.x * p.rp + r) * kEmbRows;
-  const int c = (blockIdx.y * p.lpr + sub) * V;
-  if (r >= p.rp || c >= p.F) return;
+  const int cw = (blockIdx.y * p.lpr + sub) * V, c = min(cw, p.F - V);
+  if (r >= p.rp || cw >= p.F) return;
   float zero[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) zero[v] = 0.0f;
@@ -202,7 +237,7 @@ struct Lanes {
 };
 Lanes lanes_of(int64_t F, int V) {
   Lanes l;
-  const int64_t n = F / V;
+  const int64_t n = (F + V - 1) / V;
   l.lpr = (int)std::min<int64_t>(n, kEmbThreads);
   l.rp = kEmbThreads / l.lpr;
   l.slabs = (unsigned)((n + l.lpr - 1) / l.lpr);
@@ -228,13 +263,8 @@ int launch_embed_cols(const Embed& a, int* err, hipStream_t s) {
 
 template <typename T>
 int launch_embed_type(const Embed& a, int* err, hipStream_t s) {
-  const auto fit = [&](int v) {
-    return cols_fit<T>(v, a.table, a.ldt, a.F) && cols_fit<T>(v, a.out, a.F, a.F);
-  };
-  if constexpr (sizeof(T) == 2)
-    if (fit(8)) return launch_embed_cols<T, 8>(a, err, s);
-  if (fit(4)) return launch_embed_cols<T, 4>(a, err, s);
-  return launch_embed_cols<T, 1>(a, err, s);
+  return a.F >= vector_cols<T>() ? launch_embed_cols<T, vector_cols<T>()>(a, err, s)
+                                 : launch_embed_cols<T, 1>(a, err, s);
 }
 
 template <typename T, int V>
@@ -255,13 +285,7 @@ int launch_grad_cols(EmbedGrad p, hipStream_t s) {
 
 template <typename T>
 int launch_grad_type(const EmbedGrad& p, hipStream_t s) {
-  const auto fit = [&](int v) {
-    return cols_fit<T>(v, p.dout, p.F, p.F) && cols_fit<T>(v, p.dtable, p.F, p.F);
-  };
-  if constexpr (sizeof(T) == 2)
-    if (fit(8)) return launch_grad_cols<T, 8>(p, s);
-  if (fit(4)) return launch_grad_cols<T, 4>(p, s);
-  return launch_grad_cols<T, 1>(p, s);
+  return p.F >= vector_cols<T>() ? launch_grad_cols<T, vector_cols<T>()>(p, s) : launch_grad_cols<T, 1>(p, s);
 }
 
 struct EmbedLayout {

@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kNormTile = 128;  // rows of a tile
-constexpr int kU = 4;           // rows in flight per thread
+constexpr int kU = 4;           // rows in flight per thread (eight: fewer wavefronts, 62 -> 78 us)
 
 struct NormArgs {
   const void *x, *gi, *gamma, *beta, *dout;
@@ -455,14 +455,20 @@ __global__ __launch_bounds__(kWave) void norm_params(const double* __restrict__ 
                                                      T* __restrict__ dgamma, T* __restrict__ dbeta) {
   const int i = blockIdx.x * kWave + threadIdx.x, c = i / 2;
   if (c >= F) return;
-  double acc[4] = {};
-  for (int r = 0; r < groups; r += 4) {
+  double acc[16] = {};
+  for (int r = 0; r < groups; r += 16) {
+    double x[16];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (r + u < groups) acc[u] += sums[((int64_t)(r + u) * F + c) * 2 + i % 2];
+    for (int u = 0; u < 16; ++u) x[u] = sums[((int64_t)min(r + u, groups - 1) * F + c) * 2 + i % 2];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) acc[u] += r + u < groups ? x[u] : 0.0;
   }
   T* to = i % 2 ? dgamma : dbeta;
-  if (to != nullptr) to[c] = (T)((acc[0] + acc[1]) + (acc[2] + acc[3]));
+#pragma unroll
+  for (int h = 8; h > 0; h >>= 1)
+#pragma unroll
+    for (int u = 0; u < h; ++u) acc[u] += acc[u + h];
+  if (to != nullptr) to[c] = (T)acc[0];
 }
 
 constexpr int kNormWaves = 4096;  // wavefronts over graphs: sixteen a CU
@@ -480,7 +486,7 @@ struct NormLayout {
   size_t goff, err, sums, groups, coef, cols, total;
   int64_t rows;  // of sums, at most
 };
-// For any alignment: the larger of what the two ways need.
+// For any way that the width may take.
 NormLayout norm_layout(int64_t Nb, int64_t F, int64_t G, int64_t K, bool bwd) {
   NormLayout L;
   const int64_t tiles = Nb / kNormTile + G, waves = std::min<int64_t>(G, kNormWaves);
@@ -529,17 +535,12 @@ int launch_norm_cols(NormArgs& p, int index_type, int64_t* rows, hipStream_t s) 
 
 template <typename T, bool BWD>
 int launch_norm_type(NormArgs& p, const GroupNorm& n, int* goff, int* err, int64_t* rows, hipStream_t s) {
-  const auto fit = [&](int v) {
-    return cols_fit<T>(v, p.x, p.ldx, p.F) &&
-           (BWD ? cols_fit<T>(v, p.dout, p.F, p.F) && cols_fit<T>(v, p.dx, p.F, p.F)
-                : cols_fit<T>(v, p.out, p.F, p.F));
-  };
-  const bool four = fit(4);
+  const bool four = p.F % 4 == 0;
   const int way = by_graph(p.Nb, p.F, p.G, four);
   if (way == 0 || err != nullptr)
     if (int rc = launch_segment_bounds(n.graph_index, n.index_type, n.Nb, n.G, goff, err, s)) return rc;
   if constexpr (sizeof(T) == 2)
-    if (way == 0 && fit(8)) return launch_norm_cols<T, 8, BWD>(p, n.index_type, rows, s);
+    if (way == 0 && p.F % 8 == 0) return launch_norm_cols<T, 8, BWD>(p, n.index_type, rows, s);
   if (four) return launch_norm_cols<T, 4, BWD>(p, n.index_type, rows, s);
   return launch_norm_cols<T, 1, BWD>(p, n.index_type, rows, s);
 }
