@@ -39,6 +39,62 @@ __device__ __forceinline__ Span find_span(const AttnShape& a, const int* off, in
   return s;
 }
 
+// Beside the launch over small graphs (attention_small.h), kRestBlocks blocks take the tiles
+// of the graphs that have more than `small` queries or keys: block b the tiles b, +
+// kRestBlocks, .. in the graphs' order. 64 lanes look at 64 graphs at a time, and a block
+// goes on where it was. A batch without such graphs is seen at once, by all threads.
+constexpr int kRestBlocks = 512;
+__device__ __forceinline__ bool any_rest(const AttnShape& a, int small) {
+  bool any = false;
+  for (int g0 = 0; g0 < a.G; g0 += 16 * (int)blockDim.x) {
+    int q[16][2], k[16][2];
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const int g = min(g0 + u * (int)blockDim.x + (int)threadIdx.x, a.G - 1);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        q[u][e] = a.qoff[g + e];
+        k[u][e] = a.koff[g + e];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 16; ++u)
+      any = any || clamp_off(q[u][1], a.Nq) - clamp_off(q[u][0], a.Nq) > small ||
+            clamp_off(k[u][1], a.Nk) - clamp_off(k[u][0], a.Nk) > small;
+  }
+  return __syncthreads_or(any) != 0;
+}
+struct RestScan {
+  int base = 0, count = 0;  // graphs before base have `count` tiles
+};
+template <int TILE, bool KEYS>
+__device__ __forceinline__ Span next_span(const AttnShape& a, int grp, int small, int index, RestScan& st) {
+  for (; st.base < a.G; st.base += kWave) {
+    const int g = min(st.base + lane_id(), a.G - 1);
+    Span s;
+    s.q0 = clamp_off(a.qoff[g], a.Nq);
+    s.nq = max(clamp_off(a.qoff[g + 1], a.Nq) - s.q0, 0);
+    s.k0 = clamp_off(a.koff[g], a.Nk);
+    s.nk = max(clamp_off(a.koff[g + 1], a.Nk) - s.k0, 0);
+    const bool rest = st.base + lane_id() < a.G && (s.nq > small || s.nk > small);
+    const int64_t rows = KEYS ? (int64_t)s.nk : (int64_t)s.nq * grp;
+    const int tiles = rest ? (int)((rows + TILE - 1) / TILE) : 0;
+    const int incl = wave_incl_scan(tiles), total = __shfl(incl, kWave - 1);
+    if (index < st.count + total) {
+      const int l = uniform(__ffsll((long long)__ballot(index < st.count + incl)) - 1);
+      s.g = uniform(st.base + l);
+      s.tile = uniform(index - st.count - __shfl(incl - tiles, l));
+      s.q0 = uniform(__shfl(s.q0, l));
+      s.nq = uniform(__shfl(s.nq, l));
+      s.k0 = uniform(__shfl(s.k0, l));
+      s.nk = uniform(__shfl(s.nk, l));
+      return s;
+    }
+    st.count = uniform(st.count + total);
+  }
+  return Span{-1, 0, 0, 0, 0, 0};
+}
+
 // The distance bytes [nq, nk] of a span's graph, or NULL where they would not
 // lie inside the array (every pair is then masked).
 __device__ __forceinline__ const uint8_t* dist_block(const AttnShape& a, const Span& s) {

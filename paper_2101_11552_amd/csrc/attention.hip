@@ -11,7 +11,7 @@ namespace {
 int key_parts(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t Hk) {
   if (G < 1 || Nq < 1 || small_graphs(Nq, Nk, G, Hk)) return 1;
   const int64_t grp = H / Hk, rows = Nq * grp / G;
-  const int64_t tile = rows <= 16 ? 16 : rows <= 192 ? 64 : 128;
+  const int64_t tile = rows <= 16 ? 16 : 64;
   const int64_t blocks = G * ((rows + tile - 1) / tile) * Hk;
   const int64_t keys = Nk / G;
   return (int)std::max<int64_t>(std::min<int64_t>({1024 / std::max<int64_t>(blocks, 1), keys / 256, kKeyParts}), 1);

@@ -38,7 +38,7 @@ struct AttnFwd {
 };
 
 // CAP: 0 none, 1 capped scores, 2 bounded ones (capped at kBoundedCap at most, no bias).
-template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, int CAP>
+template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, int CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDV = BN + lds_pad<T>();
@@ -55,12 +55,16 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
   const int per_slot = (a.Hk + p.heads - 1) / p.heads;
-  const int64_t slot = blockIdx.x / per_slot;
+  const int slot = (int)(blockIdx.x / per_slot);
   const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
-  const Span s = find_span<BM>(a, a.qoff, a.Nq, grp, slot);
+  RestScan scan;
+  if (REST && !any_rest(a, p.small)) return;
+  for (int index = slot;; index += kRestBlocks) {
+  const Span s = REST ? next_span<BM, false>(a, grp, p.small, index, scan)
+                      : find_span<BM>(a, a.qoff, a.Nq, grp, slot);
   const int64_t M = (int64_t)s.nq * grp;
   const int64_t r0 = (int64_t)s.tile * BM;
-  if (s.g < 0 || r0 >= M || (s.nq <= p.small && s.nk <= p.small)) return;
+  if (s.g < 0 || r0 >= M) return;
   const int lane = lane_id(), col = lane & 15, g = lane >> 4;
   const int wave = uniform((int)threadIdx.x / kWave);
   const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
@@ -300,6 +304,8 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
         p.lse[row] = l[t] == 0.0f ? -INFINITY : mu + log2f(l[t]) * kLn2;
     }
   }
+  if (!REST) return;
+  }
 }
 
 // Joins the parts of each (query, head): W wavefronts a row, lane i of each with part i's
@@ -365,23 +371,24 @@ __global__ __launch_bounds__(kBlock) void attn_join(AttnFwd p) {
   }
 }
 
-template <typename T, int DP, int WAVES, int QT, int VEC>
+template <typename T, int DP, int WAVES, int QT, int VEC, bool REST = false>
 int launch_fwd(AttnFwd& p, hipStream_t s) {
   constexpr int BM = WAVES * QT * 16;
   const int grp = p.a.H / p.a.Hk;
-  const int64_t slots = (int64_t)p.a.Nq * grp / BM + p.a.G;
+  const int64_t slots = REST ? kRestBlocks : (int64_t)p.a.Nq * grp / BM + p.a.G;
+  if ((int64_t)p.a.Nq * grp / BM + p.a.G >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
   const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
   const dim3 grid((unsigned)blocks, (unsigned)p.nsplit);
   const size_t lds = bias_table_bytes(p.a);
   const int cap = p.a.cap <= 0.0f ? 0 : p.a.B > 0 || p.a.cap > kBoundedCap ? 1 : 2;
   if (p.a.B > 0) {
-    if (cap) attn_fwd<T, DP, WAVES, QT, VEC, true, 1><<<grid, WAVES * kWave, lds, s>>>(p);
-    else attn_fwd<T, DP, WAVES, QT, VEC, true, 0><<<grid, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_fwd<T, DP, WAVES, QT, VEC, true, 1, REST><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, VEC, true, 0, REST><<<grid, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap == 2) attn_fwd<T, DP, WAVES, QT, VEC, false, 2><<<grid, WAVES * kWave, lds, s>>>(p);
-    else if (cap) attn_fwd<T, DP, WAVES, QT, VEC, false, 1><<<grid, WAVES * kWave, lds, s>>>(p);
-    else attn_fwd<T, DP, WAVES, QT, VEC, false, 0><<<grid, WAVES * kWave, lds, s>>>(p);
+    if (cap == 2) attn_fwd<T, DP, WAVES, QT, VEC, false, 2, REST><<<grid, WAVES * kWave, lds, s>>>(p);
+    else if (cap) attn_fwd<T, DP, WAVES, QT, VEC, false, 1, REST><<<grid, WAVES * kWave, lds, s>>>(p);
+    else attn_fwd<T, DP, WAVES, QT, VEC, false, 0, REST><<<grid, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_fwd");
   if (p.nsplit > 1) {

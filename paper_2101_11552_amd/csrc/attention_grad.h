@@ -104,8 +104,13 @@ __device__ __forceinline__ void add_to_bins(float* bin, const unsigned (&b)[4], 
   for (int i = 0; i < 4; ++i) bin[b[i] * kWave] = r[i];
 }
 
-template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP>
-__global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
+// Two wavefronts a SIMD where one tile each leaves registers for them.
+template <typename T, int DP, int TILES> constexpr int grad_waves() {
+  return TILES == 1 && DP * sizeof(T) <= 256 ? 2 : 1;
+}
+
+template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP, bool REST>
+__global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn_grad_q(AttnGrad p) {
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BN + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
@@ -121,18 +126,27 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
   const int per_slot = (a.Hk + p.heads - 1) / p.heads;
-  const int64_t slot = blockIdx.x / per_slot;
+  const int slot = (int)(blockIdx.x / per_slot);
   const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
   const int kvh1 = min(kvh0 + p.heads, a.Hk);
   const bool want_bias = BIAS && p.bias_part != nullptr;
   float* bins = tab + grp * (a.B + 1);  // [WAVES][copies][B + 1][64], one column a lane
-  const Span s = find_span<BM>(a, a.qoff, a.Nq, grp, slot);
+  float* bpart = want_bias ? p.bias_part + (int64_t)slot * a.H * a.B : nullptr;
+  const auto no_bias = [&]() {
+    for (int i = threadIdx.x; i < (kvh1 - kvh0) * grp * a.B; i += THREADS) bpart[kvh0 * grp * a.B + i] = 0.0f;
+  };
+  RestScan scan;
+  if (REST) {
+    if (want_bias) no_bias();  // (the rest's tiles add to their block's row)
+    if (!any_rest(a, p.small)) return;
+  }
+  for (int index = slot;; index += kRestBlocks) {
+  const Span s = REST ? next_span<BM, false>(a, grp, p.small, index, scan)
+                      : find_span<BM>(a, a.qoff, a.Nq, grp, slot);
   const int64_t M = (int64_t)s.nq * grp;
   const int64_t r0 = (int64_t)s.tile * BM;
-  if (s.g < 0 || r0 >= M || (s.nq <= p.small && s.nk <= p.small)) {
-    if (want_bias)
-      for (int i = threadIdx.x; i < (kvh1 - kvh0) * grp * a.B; i += THREADS)
-        p.bias_part[(slot * a.H + (int64_t)kvh0 * grp) * a.B + i] = 0.0f;
+  if (s.g < 0 || r0 >= M) {
+    if (!REST && want_bias) no_bias();
     return;
   }
   const int lane = lane_id(), col = lane & 15, g = lane >> 4;
@@ -412,7 +426,10 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) sum += bins[(w * (a.B + 1) + b) * kWave + lane];
         for (int o = kWave / 2; o >= grp; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane < grp) p.bias_part[(slot * a.H + (int64_t)kvh * grp + lane) * a.B + b] = sum;
+        if (lane < grp) {
+          float* to = bpart + (kvh * grp + lane) * a.B + b;
+          *to = REST ? *to + sum : sum;
+        }
       }
       continue;
     }
@@ -426,8 +443,11 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_q(AttnGrad p) {
           if ((base + (ln & 15)) % grp == h) sum += bins[(w * (a.B + 1) + b) * kWave + ln];
         }
       }
-      p.bias_part[(slot * a.H + (int64_t)kvh * grp) * a.B + i] = sum;
+      float* to = bpart + kvh * grp * a.B + i;
+      *to = REST ? *to + sum : sum;
     }
+  }
+  if (!REST) return;
   }
 }
 
@@ -443,8 +463,8 @@ __device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
   return (lo & 0xFFFFu) | (hi << 16);
 }
 
-template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP>
-__global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
+template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP, bool REST>
+__global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn_grad_kv(AttnGrad p) {
   constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BR + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, XT = BR / 16;
@@ -460,11 +480,15 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
   const int per_slot = (a.Hk + p.heads - 1) / p.heads;
-  const int64_t slot = blockIdx.x / per_slot;
+  const int slot = (int)(blockIdx.x / per_slot);
   const int kvh0 = (int)(blockIdx.x % per_slot) * p.heads;
-  const Span s = find_span<BK>(a, a.koff, a.Nk, 1, slot);
+  RestScan scan;
+  if (REST && !any_rest(a, p.small)) return;
+  for (int index = slot;; index += kRestBlocks) {
+  const Span s = REST ? next_span<BK, true>(a, grp, p.small, index, scan)
+                      : find_span<BK>(a, a.koff, a.Nk, 1, slot);
   const int64_t kt0 = (int64_t)s.tile * BK;
-  if (s.g < 0 || kt0 >= s.nk || (s.nq <= p.small && s.nk <= p.small)) return;
+  if (s.g < 0 || kt0 >= s.nk) return;
   const int lane = lane_id(), col = lane & 15, g = lane >> 4;
   const int wave = uniform((int)threadIdx.x / kWave);
   const uint8_t* dist = BIAS ? dist_block(a, s) : nullptr;
@@ -661,6 +685,8 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_grad_kv(AttnGrad p) {
       }
     }
   }
+  if (!REST) return;
+  }
 }
 
 // The parts of dk and dv added in order, an element a thread. Keys outside every graph
@@ -683,7 +709,7 @@ __global__ __launch_bounds__(kBlock) void attn_grad_join(AttnGrad p) {
 
 // Tiles of rows and keys that the two passes take.
 struct RowPlan {
-  int waves, qt, copies, kt, nsplit;
+  int waves, qt, copies, nsplit;
   int64_t slots;
   int small_waves, small_block;  // of the launch over small graphs (0: none)
   size_t small_lds;              // a wavefront's
@@ -692,7 +718,7 @@ inline size_t bins_bytes(int waves, int copies, int64_t B) {
   return sizeof(float) * (size_t)waves * copies * (B + 1) * kWave;
 }
 
-template <typename T, int DP, int WAVES, int QT, int VEC>
+template <typename T, int DP, int WAVES, int QT, int VEC, bool REST = false>
 int launch_grad_q(const AttnGrad& p, int64_t slots, hipStream_t s) {
   const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many query tiles");
@@ -700,28 +726,29 @@ int launch_grad_q(const AttnGrad& p, int64_t slots, hipStream_t s) {
   const bool cap = p.a.cap > 0.0f;
   const unsigned n = (unsigned)blocks;
   if (p.a.B > 0) {
-    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, true, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_q<T, DP, WAVES, QT, VEC, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, true, true, REST><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, VEC, true, false, REST><<<n, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, false, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_q<T, DP, WAVES, QT, VEC, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_q<T, DP, WAVES, QT, VEC, false, true, REST><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_q<T, DP, WAVES, QT, VEC, false, false, REST><<<n, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_grad_q");
   return TFG_OK;
 }
-template <typename T, int DP, int WAVES, int KT, int VEC>
+template <typename T, int DP, int WAVES, int KT, int VEC, bool REST = false>
 int launch_grad_kv(const AttnGrad& p, hipStream_t s) {
-  const int64_t blocks = ((int64_t)p.a.Nk / (WAVES * KT * 16) + p.a.G) * ((p.a.Hk + p.heads - 1) / p.heads);
+  const int64_t slots = REST ? kRestBlocks : (int64_t)p.a.Nk / (WAVES * KT * 16) + p.a.G;
+  const int64_t blocks = slots * ((p.a.Hk + p.heads - 1) / p.heads);
   if (blocks >= (int64_t(1) << 31)) return fail(TFG_ERR_TOO_LARGE, "too many key tiles");
   const size_t lds = bias_table_bytes(p.a);
   const bool cap = p.a.cap > 0.0f;
   const dim3 n((unsigned)blocks, (unsigned)p.nsplit);
   if (p.a.B > 0) {
-    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, true, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_kv<T, DP, WAVES, KT, VEC, true, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, true, true, REST><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, VEC, true, false, REST><<<n, WAVES * kWave, lds, s>>>(p);
   } else {
-    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, false, true><<<n, WAVES * kWave, lds, s>>>(p);
-    else attn_grad_kv<T, DP, WAVES, KT, VEC, false, false><<<n, WAVES * kWave, lds, s>>>(p);
+    if (cap) attn_grad_kv<T, DP, WAVES, KT, VEC, false, true, REST><<<n, WAVES * kWave, lds, s>>>(p);
+    else attn_grad_kv<T, DP, WAVES, KT, VEC, false, false, REST><<<n, WAVES * kWave, lds, s>>>(p);
   }
   TFG_LAUNCHED("attn_grad_kv");
   if (p.nsplit > 1) {

@@ -7,34 +7,40 @@ namespace {
 
 constexpr size_t kMaxLds = 160 << 10;
 
-// Larger tiles where they still fill the card, which takes some kBlocks blocks: two row
-// (key) tiles a wavefront read each staged tile twice from LDS for four products. Heads
-// of more than 64 columns keep one: two take all registers of a SIMD for one wavefront.
+// A launch that fills the card has some kBlocks blocks.
 constexpr int64_t kBlocks = 768;
+
+// Two row tiles a wavefront read each staged tile of keys once for both, where that costs
+// no wavefront a SIMD (bf16 heads of 33 to 64 columns: two wavefronts either way, 455 -> 425
+// us for 96 graphs of 100 to 500 nodes, 8 heads; float32 of up to 16, 666 -> 609) and the
+// blocks still fill the card. Elsewhere it does (bf16 of 17 to 32: three to two, 295 -> 324).
+// Two key tiles a wavefront always do, or gain nothing.
+bool two_row_tiles(int float_type, int64_t D) {
+  return float_type == TFG_BF16 ? D > 32 && D <= 64 : D <= 16;
+}
 
 RowPlan row_plan(const AttnShape& a, int float_type, bool want_bias) {
   const int64_t Nq = a.Nq, Nk = a.Nk, G = a.G, H = a.H, Hk = a.Hk, D = a.D, B = a.B;
   const int64_t grp = H / Hk, graphs = std::max<int64_t>(G, 1), rows = Nq * grp / graphs;
-  RowPlan r{1, 1, 1, 1, 1, 0, 0, 0, 0};
+  RowPlan r{1, 1, 1, 1, 0, 0, 0, 0};
   const SmallPlan sp = small_grad_plan(float_type, a, want_bias);
   r.small_waves = sp.waves;
   r.small_block = sp.per_block;
   r.small_lds = sp.lds;
-  if (sp.waves > 0 || (rows > 192 && D <= 64 && rows / 128 * graphs * Hk >= kBlocks)) r.waves = 4, r.qt = 2;
-  else if (rows > 16) r.waves = 4;
+  if (rows > 16 || sp.waves > 0) r.waves = 4;
+  if (sp.waves == 0 && rows > 192 && two_row_tiles(float_type, D) && D % (float_type == TFG_BF16 ? 8 : 4) == 0 && rows / 128 * graphs * Hk >= kBlocks) r.qt = 2;
   if (16 % grp != 0) r.copies = r.qt;
   // the LDS of the tiles (three of 64 x DP bf16 or 32 x DP float32), the bias table and the bins
   const int64_t DP = D <= 16 ? 16 : D <= 32 ? 32 : D <= 64 ? 64 : 128;
   const size_t tiles = 3 * 2 * 64 * (size_t)(DP + 16) + 2 * 8 * (size_t)DP;
   if (tiles + sizeof(float) * (size_t)(grp * (B + 1)) + bins_bytes(r.waves, r.copies, B) > kMaxLds)
     r.waves = r.qt = r.copies = 1;
-  r.slots = Nq * grp / (r.waves * r.qt * 16) + G;
+  r.slots = sp.waves > 0 ? kRestBlocks : Nq * grp / (r.waves * r.qt * 16) + G;
   const int64_t keys = Nk / graphs;
-  if (sp.waves > 0 || (keys > 192 && D <= 64 && keys / 128 * graphs * Hk >= kBlocks)) r.kt = 2;
   // the queries of a key tile in parts of at least four tiles of rows
-  const int64_t blocks = std::max<int64_t>(keys / (64 * r.kt), 1) * graphs * Hk;
+  const int64_t blocks = std::max<int64_t>(keys / 64, 1) * graphs * Hk;
   const int64_t tiles_of_rows = (Nq / graphs + 63) / 64 * grp;
-  r.nsplit = (int)std::max<int64_t>(std::min<int64_t>({kBlocks / blocks, tiles_of_rows / 4, 16}), 1);
+  if (sp.waves == 0) r.nsplit = (int)std::max<int64_t>(std::min<int64_t>({kBlocks / blocks, tiles_of_rows / 4, 16}), 1);
   return r;
 }
 

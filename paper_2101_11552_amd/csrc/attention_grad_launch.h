@@ -26,19 +26,26 @@ int launch_grad_width(AttnGrad& p, const RowPlan& r, hipStream_t s) {
       if (int rc = launch_grad_small<T, DP>(q, SmallPlan{r.small_waves, r.small_block, r.small_lds}, s)) return rc;
       p.small = kSmallGraph;  // the rest: graphs with more nodes, few if any
       p.heads = p.a.Hk;
+      if (r.waves == 1) {
+        if (int rc = launch_grad_q<T, DP, 1, 1, 0, true>(p, r.slots, s)) return rc;
+      } else if (int rc = launch_grad_q<T, DP, 4, 1, 8, true>(p, r.slots, s)) {
+        return rc;
+      }
+      return launch_grad_kv<T, DP, 4, 1, 8, true>(p, s);
     }
   }
   const bool whole = whole_vectors<T>(D);
   if (p.a.Nq > 0) {
     int rc;
-    if (r.qt == 2) rc = whole ? launch_grad_q<T, DP, 4, 2, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 2, 0>(p, r.slots, s);
-    else if (r.waves == 4) rc = whole ? launch_grad_q<T, DP, 4, 1, 8>(p, r.slots, s) : launch_grad_q<T, DP, 4, 1, 0>(p, r.slots, s);
-    else rc = launch_grad_q<T, DP, 1, 1, 0>(p, r.slots, s);
+    constexpr int QT = (sizeof(T) == 2 ? DP == 64 : DP == 16) ? 2 : 1;  // (the plan's widths)
+    if (r.waves == 1) rc = launch_grad_q<T, DP, 1, 1, 0>(p, r.slots, s);
+    else if (!whole) rc = launch_grad_q<T, DP, 4, 1, 0>(p, r.slots, s);
+    else if (r.qt == 2) rc = launch_grad_q<T, DP, 4, QT, 8>(p, r.slots, s);
+    else rc = launch_grad_q<T, DP, 4, 1, 8>(p, r.slots, s);
     if (rc) return rc;
   }
   if (p.a.Nk == 0) return TFG_OK;
   if (!whole) return launch_grad_kv<T, DP, 4, 1, 0>(p, s);
-  if (r.kt == 2) return launch_grad_kv<T, DP, 4, 2, 8>(p, s);
   return launch_grad_kv<T, DP, 4, 1, 8>(p, s);
 }
 

@@ -5,7 +5,11 @@
 
 namespace tfg {
 
-// Tiles of rows: 128 where graphs have many, 64, or 16 for a few queries each.
+// Tiles of 64 rows, or of 16 for a few queries each. Of 128, two row tiles a wavefront, for
+// bf16 heads of 33 to 64 columns and graphs of a thousand rows and more: two wavefronts a
+// SIMD either way there (three graphs of 4,000 to 9,000 nodes, 8 heads of 64, 556 -> 526 us;
+// 96 graphs of 100 to 500: 120 -> 129; other widths lose a wavefront: 16 columns 377 -> 383,
+// 128 905 -> 1,020).
 template <typename T, int DP>
 int launch_fwd_rows(AttnFwd& p, hipStream_t s) {
   const int64_t rows = (int64_t)p.a.Nq * (p.a.H / p.a.Hk) / std::max(p.a.G, 1);
@@ -14,17 +18,18 @@ int launch_fwd_rows(AttnFwd& p, hipStream_t s) {
   p.vec_o = row_vector<T>(p.out, (int64_t)p.a.H * D, D);
   p.heads = 1;
   p.small = 0;
-  if (p.nsplit == 1 && whole_vectors<T>(D) && small_graphs(p.a.Nq, p.a.Nk, p.a.G, p.a.Hk)) {
+  const bool whole = whole_vectors<T>(D);
+  if (p.nsplit == 1 && whole && small_graphs(p.a.Nq, p.a.Nk, p.a.G, p.a.Hk)) {
     if (int rc = launch_small<T, DP>(p, s)) return rc;
     p.small = kSmallGraph;  // the rest: graphs with more nodes, few if any
     p.heads = p.a.Hk;
-    return launch_fwd<T, DP, 4, 2, 8>(p, s);
+    return launch_fwd<T, DP, 4, 1, 8, true>(p, s);
   }
-  if (!whole_vectors<T>(D))
-    return rows <= 16 ? launch_fwd<T, DP, 1, 1, 0>(p, s) : launch_fwd<T, DP, 4, 1, 0>(p, s);
+  if (!whole) return rows <= 16 ? launch_fwd<T, DP, 1, 1, 0>(p, s) : launch_fwd<T, DP, 4, 1, 0>(p, s);
   if (rows <= 16) return launch_fwd<T, DP, 1, 1, 8>(p, s);
-  if (rows <= 192) return launch_fwd<T, DP, 4, 1, 8>(p, s);
-  return launch_fwd<T, DP, 4, 2, 8>(p, s);
+  if constexpr (DP == 64 && sizeof(T) == 2)
+    if (rows >= 1024 && rows / 128 * p.a.G * p.a.Hk >= 768) return launch_fwd<T, DP, 4, 2, 8>(p, s);
+  return launch_fwd<T, DP, 4, 1, 8>(p, s);
 }
 
 // Heads of at most 32 columns, and wider ones (translation units of their own).
