@@ -13,7 +13,7 @@
 // products instead of five, and no partial dq in memory.
 //
 // delta from a bf16 output carries that output's rounding, which short rows feel
-// (a node's weights are large there): up to two tiles of keys it is summed from p
+// (a node's weights are large there): up to 128 keys it is summed from p
 // and dp in a first sweep instead. The same sweep serves rows whose log-sum is so
 // large (a bias of the type's lowest value) that u - lse has lost the sum: it keeps
 // the maximum and the sum apart.
@@ -111,7 +111,10 @@ template <typename T, int DP, int TILES> constexpr int grad_waves() {
 
 template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn_grad_q(AttnGrad p) {
-  constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
+  // keys of a tile: as many as leave LDS for two blocks a CU beside the bias's bins
+  // (width 128, two graphs of 3,000 nodes, 8 heads on 2: 408 us with tiles of 32 keys, 493
+  // with 64; without a bias or a cap the whole gradient takes 566 us with 64, 652 with 32)
+  constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 && !(BIAS && DP == 128) ? 64 : 32;
   constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BN + lds_pad<T>();
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
   using U = Units<BN, DP>;
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
         again = again || (BIAS && ls != -INFINITY && fabsf(ls) > kLongLse);
       }
     }
-    again = (sizeof(T) == 2 && tiles <= 2) || (BIAS && __syncthreads_or(again));
+    again = (sizeof(T) == 2 && s.nk <= 128) || (BIAS && __syncthreads_or(again));
 
     x8_t<T> kr[KU][4], vr[VU];
     unsigned bk[QT][KT];
