@@ -214,17 +214,4 @@ struct Units {
   static __device__ __forceinline__ int quad_col(int c) { return (c / (ROWS / 4)) * 8; }
 };
 
-// Four rows of eight columns to LDS as columns, places interleaved (see tiles.h).
-template <typename T, int LD>
-__device__ __forceinline__ void put_columns(T* dst, int quad, int d0, const x8_t<T> (&v)[4]) {
-  const int place = interleaved_quad(quad);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    x4_t<T> w;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = v[i][e];
-    *reinterpret_cast<x4_t<T>*>(dst + (d0 + e) * LD + place) = w;
-  }
-}
-
 }  // namespace tfg

@@ -41,7 +41,9 @@ struct AttnFwd {
 template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, int CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 ? 64 : 32;
-  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDV = BN + lds_pad<T>();
+  constexpr int THREADS = WAVES * kWave;
+  using KTile = Tile<T, DP>;
+  using VTile = Tile<T, BN>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
   using U = Units<BN, DP>;
   // staging units of a thread: rows of eight columns (K), four rows of eight (V)
@@ -49,8 +51,8 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
   constexpr int VU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
   // the next tile waits in registers where it takes at most 48 of them
   constexpr bool AHEAD = VEC == 8 && (KU * 8 + VU * 32) * sizeof(T) / 4 <= 48;
-  __shared__ T Ks[BN * LDK];
-  __shared__ T Vt[DP * LDV];
+  __shared__ T Ks[BN * KTile::LD];
+  __shared__ T Vt[DP * VTile::LD];
   extern __shared__ float tab[];
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
@@ -157,12 +159,12 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
 #pragma unroll
       for (int u = 0; u < KU; ++u) {
         const int c = u * THREADS + threadIdx.x;
-        if (U::row8(c) < BN) put8<T>(Ks + U::row8(c) * LDK + U::col8(c), kr[u]);
+        if (U::row8(c) < BN) KTile::put8(Ks, U::row8(c), U::col8(c), kr[u]);
       }
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
         const int c = u * THREADS + threadIdx.x;
-        if (U::quad_col(c) < DP) put_columns<T, LDV>(Vt, U::quad(c), U::quad_col(c), vr[u]);
+        if (U::quad_col(c) < DP) VTile::put_columns(Vt, U::quad(c), U::quad_col(c), vr[u]);
       }
       __syncthreads();
       if (AHEAD && kt + 1 < t1) fetch(kt + 1);
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
         for (int t = 0; t < QT; ++t) sc[t][x] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
-          const frag_t<T, DP> kf = lds_frag<T, DP>(Ks + (x * 16 + col) * LDK, c, g);
+          const frag_t<T, DP> kf = KTile::frag(Ks, x * 16 + col, c, g);
 #pragma unroll
           for (int t = 0; t < QT; ++t) sc[t][x] = mma(kf, qf[t][c], sc[t][x]);
         }
@@ -270,7 +272,7 @@ __global__ __launch_bounds__(WAVES * kWave) void attn_fwd(AttnFwd p) {
         for (int t = 0; t < QT; ++t) pf[t] = as_operand<T>(sc[t][2 * x], sc[t][2 * x + 1]);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const x8_t<T> vf = lds8<T>(Vt + (d * 16 + col) * LDV + x * 32 + g * 8);
+          const x8_t<T> vf = VTile::get8(Vt, d * 16 + col, x * 32 + g * 8);
 #pragma unroll
           for (int t = 0; t < QT; ++t) o[t][d] = mma(vf, pf[t], o[t][d]);
         }

@@ -109,22 +109,30 @@ template <typename T, int DP, int TILES> constexpr int grad_waves() {
   return TILES == 1 && DP * sizeof(T) <= 256 ? 2 : 1;
 }
 
+// Whether the row tiles' chunks change places (see Tile): in wider heads, and for the
+// column tiles, the addresses' registers cost more than the conflicts (4 graphs of 1,500, 8
+// heads on 4, bf16, no bias: 97 -> 91 us at width 16, 103 -> 99 at 32, but 198 -> 213 at 64;
+// column tiles too, width 32 with a bias: 170 -> 218, a wavefront a SIMD less).
+template <typename T, int DP> constexpr bool swapped_chunks() { return sizeof(T) == 2 && DP <= 32; }
+
 template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn_grad_q(AttnGrad p) {
   // keys of a tile: as many as leave LDS for two blocks a CU beside the bias's bins
   // (width 128, two graphs of 3,000 nodes, 8 heads on 2: 408 us with tiles of 32 keys, 493
   // with 64; without a bias or a cap the whole gradient takes 566 us with 64, 652 with 32)
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 && !(BIAS && DP == 128) ? 64 : 32;
-  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BN + lds_pad<T>();
+  constexpr int THREADS = WAVES * kWave;
+  using Rows = Tile<T, DP, swapped_chunks<T, DP>()>;
+  using Columns = Tile<T, BN, false>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
   using U = Units<BN, DP>;
   // staging units of a thread: four rows of eight columns (K), rows of eight (V)
   constexpr int KU = (BN / 4 * (DP / 8) + THREADS - 1) / THREADS;
   constexpr int VU = (BN * (DP / 8) + THREADS - 1) / THREADS;
   constexpr bool AHEAD = VEC == 8 && (KU * 32 + VU * 8) * sizeof(T) / 4 <= 48;
-  __shared__ T Ks[BN * LDK];
-  __shared__ T Vs[BN * LDK];
-  __shared__ T Kt[DP * LDT];
+  __shared__ T Ks[BN * Rows::LD];
+  __shared__ T Vs[BN * Rows::LD];
+  __shared__ T Kt[DP * Columns::LD];
   extern __shared__ float tab[];
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
@@ -237,14 +245,14 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
         const int c = u * THREADS + threadIdx.x;
         if (U::quad_col(c) < DP) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) put8<T>(Ks + (U::quad(c) * 4 + i) * LDK + U::quad_col(c), kr[u][i]);
-          put_columns<T, LDT>(Kt, U::quad(c), U::quad_col(c), kr[u]);
+          for (int i = 0; i < 4; ++i) Rows::put8(Ks, U::quad(c) * 4 + i, U::quad_col(c), kr[u][i]);
+          Columns::put_columns(Kt, U::quad(c), U::quad_col(c), kr[u]);
         }
       }
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
         const int c = u * THREADS + threadIdx.x;
-        if (U::row8(c) < BN) put8<T>(Vs + U::row8(c) * LDK + U::col8(c), vr[u]);
+        if (U::row8(c) < BN) Rows::put8(Vs, U::row8(c), U::col8(c), vr[u]);
       }
     };
     const auto fetch_buckets = [&](int kt) {
@@ -262,8 +270,8 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
       for (int t = 0; t < QT; ++t) sc[t] = dp[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        const frag_t<T, DP> kf = lds_frag<T, DP>(Ks + (x * 16 + col) * LDK, c, g);
-        const frag_t<T, DP> vf = lds_frag<T, DP>(Vs + (x * 16 + col) * LDK, c, g);
+        const frag_t<T, DP> kf = Rows::frag(Ks, x * 16 + col, c, g);
+        const frag_t<T, DP> vf = Rows::frag(Vs, x * 16 + col, c, g);
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           sc[t] = mma(kf, qf[t][c], sc[t]);
@@ -405,7 +413,7 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const x8_t<T> kf = lds8<T>(Kt + (d * 16 + col) * LDT + x2 * 32 + g * 8);
+          const x8_t<T> kf = Columns::get8(Kt, d * 16 + col, x2 * 32 + g * 8);
 #pragma unroll
           for (int t = 0; t < QT; ++t) o[t][d] = mma(kf, sf[t], o[t][d]);
         }
@@ -469,15 +477,17 @@ __device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
 template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn_grad_kv(AttnGrad p) {
   constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
-  constexpr int THREADS = WAVES * kWave, LDK = DP + lds_pad<T>(), LDT = BR + lds_pad<T>();
+  constexpr int THREADS = WAVES * kWave;
+  using Rows = Tile<T, DP, swapped_chunks<T, DP>()>;
+  using Columns = Tile<T, BR, false>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, XT = BR / 16;
   using U = Units<BR, DP>;
   constexpr int RU = (BR / 4 * (DP / 8) + THREADS - 1) / THREADS;  // four rows of eight columns
   constexpr bool AHEAD = VEC == 8 && RU * 64 * sizeof(T) / 4 <= 64;
-  __shared__ T Qs[BR * LDK];
-  __shared__ T Os[BR * LDK];
-  __shared__ T Qt[DP * LDT];
-  __shared__ T Ot[DP * LDT];
+  __shared__ T Qs[BR * Rows::LD];
+  __shared__ T Os[BR * Rows::LD];
+  __shared__ T Qt[DP * Columns::LD];
+  __shared__ T Ot[DP * Columns::LD];
   __shared__ float rows[3][BR];  // row_a, row_c, delta
   extern __shared__ float tab[];
   const AttnShape& a = p.a;
@@ -590,11 +600,11 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn
         if (U::quad_col(c) < DP) {
 #pragma unroll
           for (int e4 = 0; e4 < 4; ++e4) {
-            put8<T>(Qs + (U::quad(c) * 4 + e4) * LDK + U::quad_col(c), qr[u][e4]);
-            put8<T>(Os + (U::quad(c) * 4 + e4) * LDK + U::quad_col(c), dr[u][e4]);
+            Rows::put8(Qs, U::quad(c) * 4 + e4, U::quad_col(c), qr[u][e4]);
+            Rows::put8(Os, U::quad(c) * 4 + e4, U::quad_col(c), dr[u][e4]);
           }
-          put_columns<T, LDT>(Qt, U::quad(c), U::quad_col(c), qr[u]);
-          put_columns<T, LDT>(Ot, U::quad(c), U::quad_col(c), dr[u]);
+          Columns::put_columns(Qt, U::quad(c), U::quad_col(c), qr[u]);
+          Columns::put_columns(Ot, U::quad(c), U::quad_col(c), dr[u]);
         }
       }
       if ((int)threadIdx.x < BR) {
@@ -617,8 +627,8 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn
           for (int t = 0; t < KT; ++t) sc[t][h] = dp[t][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
           for (int c = 0; c < KC; ++c) {
-            const frag_t<T, DP> qf = lds_frag<T, DP>(Qs + (x * 16 + col) * LDK, c, g);
-            const frag_t<T, DP> of = lds_frag<T, DP>(Os + (x * 16 + col) * LDK, c, g);
+            const frag_t<T, DP> qf = Rows::frag(Qs, x * 16 + col, c, g);
+            const frag_t<T, DP> of = Rows::frag(Os, x * 16 + col, c, g);
 #pragma unroll
             for (int t = 0; t < KT; ++t) {
               sc[t][h] = mma(qf, kf[t][c], sc[t][h]);
@@ -656,8 +666,8 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const x8_t<T> of = lds8<T>(Ot + (d * 16 + col) * LDT + x2 * 32 + g * 8);
-          const x8_t<T> qf = lds8<T>(Qt + (d * 16 + col) * LDT + x2 * 32 + g * 8);
+          const x8_t<T> of = Columns::get8(Ot, d * 16 + col, x2 * 32 + g * 8);
+          const x8_t<T> qf = Columns::get8(Qt, d * 16 + col, x2 * 32 + g * 8);
 #pragma unroll
           for (int t = 0; t < KT; ++t) {
             dv[t][d] = mma(of, pf[t], dv[t][d]);

@@ -51,14 +51,15 @@ __device__ __forceinline__ frag_t<T, DP> frag_within(const T* row, int c, int g,
 }
 
 template <typename T, int DP> constexpr int small_fwd_lds() {  // elements a wavefront, without the table
-  return DP * (kSmallGraph + lds_pad<T>());
+  return DP * Tile<T, kSmallGraph>::LD;
 }
 
 template <typename T, int DP, bool BIAS, int CAP>
 __global__ __launch_bounds__(4 * kWave) void attn_small(AttnFwd p, int waves) {
-  constexpr int LDV = kSmallGraph + lds_pad<T>(), KC = Frag<T, DP>::KC, DT = DP / 16, KT = kSmallTiles;
+  constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = kSmallTiles;
   constexpr int VU = (kSmallGraph / 4 * (DP / 8) + kWave - 1) / kWave;
   using U = Units<kSmallGraph, DP>;
+  using VTile = Tile<T, kSmallGraph>;
   extern __shared__ float dyn[];
   const AttnShape& a = p.a;
   const int grp = a.H / a.Hk, D = a.D;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(4 * kWave) void attn_small(AttnFwd p, int waves) {
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
         const int c = u * kWave + lane;
-        if (U::quad_col(c) < DP) put_columns<T, LDV>(Vt, U::quad(c), U::quad_col(c), vr[u]);
+        if (U::quad_col(c) < DP) VTile::put_columns(Vt, U::quad(c), U::quad_col(c), vr[u]);
       }
       wave_sync();
     }
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(4 * kWave) void attn_small(AttnFwd p, int waves) {
           const x8_t<T> pf = as_operand<T>(sc[2 * x], 2 * x + 1 < kts ? sc[2 * x + 1] : zero);
 #pragma unroll
           for (int d = 0; d < DT; ++d)
-            o[d] = mma(lds8<T>(Vt + (d * 16 + col) * LDV + x * 32 + g * 8), pf, o[d]);
+            o[d] = mma(VTile::get8(Vt, d * 16 + col, x * 32 + g * 8), pf, o[d]);
         }
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);

@@ -146,18 +146,8 @@ __device__ __forceinline__ x8_t<T> lds8(const T* p) {
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 }
-template <typename T>
-__device__ __forceinline__ void put8(T* p, x8_t<T> v) {
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<bf16x8*>(p) = v;
-  } else {
-    *reinterpret_cast<f32x4*>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-    *reinterpret_cast<f32x4*>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-  }
-}
 
-// Columns added to an LDS row so that the rows of a 16-lane read start in
-// different banks.
+// Columns added to an LDS row that is read one row a lane at a time.
 template <typename T> constexpr int lds_pad() { return 16 / (int)sizeof(T); }
 
 // A lane's part of a head's DP columns as an operand: KC chunks of 32 (of 16 for DP =
@@ -191,12 +181,66 @@ __device__ __forceinline__ frag_t<T, DP> load_frag(const T* row, int c, int g, i
     return load8<T>(row, c * 32 + g * 8, D, vec);
   }
 }
-// The same of a row in LDS.
-template <typename T, int DP>
-__device__ __forceinline__ frag_t<T, DP> lds_frag(const T* row, int c, int g) {
-  if constexpr (DP == 16) return *reinterpret_cast<const frag_t<T, DP>*>(row + g * 4);
-  else return lds8<T>(row + c * 32 + g * 8);
-}
+
+// A tile of LDS rows of COLS elements that operands are read from: lane l row l % 16,
+// 16 bytes at column chunk l / 16 of a step. Of 64 such lanes the LDS serves 0..3, 12..15
+// and 20..27 together, then 4..11, 16..19 and 28..31, and so on, so padded rows, without
+// conflicts among 16 neighbouring lanes, meet in these groups: 8.1 cycles a read against
+// 4.4 without conflicts. Here chunk j of a row is kept at j ^ key(row), no padding, with
+// keys that put each such group into different banks (attention forward, bf16, width 128:
+// 236 -> 200 us; float32's products take longer than its reads: padded). 16 bf16 columns
+// are read 8 bytes a lane, from padded rows.
+template <typename T, int COLS, bool SWAP = sizeof(T) == 2> struct Tile {
+  static constexpr int PER = 16 / (int)sizeof(T), CHUNKS = COLS / PER;
+  static constexpr bool PAD = !SWAP || CHUNKS == 2;
+  static constexpr int LD = PAD ? COLS + PER : COLS;
+  static __device__ __forceinline__ int key(int row) {
+    if constexpr (PAD) return 0;
+    if constexpr (CHUNKS >= 16) return row & 15;
+    // rows 0-3 and 12-15 the keys 0..3, rows 4-11 the keys 4..7: both sets are closed under
+    // ^ 1 and ^ 2, the difference between the lane groups' chunks
+    if constexpr (CHUNKS == 8) return ((row >> 1) & 1) | ((row >> 2) & 2) | ((row ^ (row >> 1)) & 4);
+    if constexpr (CHUNKS == 4) return -(row >> 2) & 3;
+    return 0;
+  }
+  static __device__ __forceinline__ int at(int row, int col) {
+    return row * LD + ((col / PER) ^ key(row)) * PER + col % PER;
+  }
+  // Eight columns from col on, a multiple of eight.
+  static __device__ __forceinline__ x8_t<T> get8(const T* tile, int row, int col) {
+    if constexpr (sizeof(T) == 2) {
+      return *reinterpret_cast<const bf16x8*>(tile + at(row, col));
+    } else {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(tile + at(row, col));
+      const f32x4 hi = *reinterpret_cast<const f32x4*>(tile + at(row, col + 4));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  static __device__ __forceinline__ void put8(T* tile, int row, int col, x8_t<T> v) {
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x8*>(tile + at(row, col)) = v;
+    } else {
+      *reinterpret_cast<f32x4*>(tile + at(row, col)) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+      *reinterpret_cast<f32x4*>(tile + at(row, col + 4)) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+    }
+  }
+  // Four rows of eight columns of another tile as columns of this one, places interleaved.
+  static __device__ __forceinline__ void put_columns(T* tile, int quad, int d0, const x8_t<T> (&v)[4]) {
+    const int place = interleaved_quad(quad);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x4_t<T> w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = v[i][e];
+      *reinterpret_cast<x4_t<T>*>(tile + at(d0 + e, place)) = w;
+    }
+  }
+  // Chunk c of lane group g of a row of this many columns as an operand.
+  static __device__ __forceinline__ frag_t<T, COLS> frag(const T* tile, int row, int c, int g) {
+    if constexpr (COLS == 16) return *reinterpret_cast<const frag_t<T, 16>*>(tile + at(row, g * 4));
+    else return get8(tile, row, c * 32 + g * 8);
+  }
+};
 
 // Two result tiles (a = 0, 1) as one operand of 32 k.
 template <typename T>
