@@ -1,6 +1,8 @@
 // Attention inside each graph of a BatchGraph (gfx950): the choice of kernels and the
 // check of offsets. The kernels are in attention_fwd.h and
 // attention_small.h.
+#include <limits>
+
 #include "attention_launch.h"
 
 namespace tfg {
@@ -29,6 +31,8 @@ int launch_attention(const AttnShape& a, int float_type, const void* q, const vo
   if (a.G == 0 || a.Nq == 0) return TFG_OK;
   AttnFwd p{};
   p.a = a;
+  // masked scores are raw products of -inf, which a scale of zero would make NaN
+  if (a.scale == 0.0f) p.a.scale = std::numeric_limits<float>::denorm_min();
   p.q = q;
   p.k = k;
   p.v = v;
