@@ -166,24 +166,29 @@ constexpr float kBoundedCap = 60.0f;
 // Scores beyond this are differences of large numbers: see the kernels.
 constexpr float kHugeScore = 1.0e37f;
 
-// Eight columns from d0 on of the row at element `at` past base (the same in every lane).
-// VEC 8: D is a multiple of 16 bytes, the row of one element (16-byte loads at any
-// address); 4: as row_vector says. Columns past D are read from the row's last ones: finite
-// where the row is, and the other operand of their product is zero.
+// Eight columns from d0 on of the row at element `at` past base (the same in every lane;
+// below 64 rows of less than 2^23 elements, so bytes fit 32 bits and the address takes one
+// register). VEC 8: D is a multiple of 16 bytes, the row of one element (16-byte loads at
+// any address); 4: D is a multiple of four. Columns past D are read from the row's last
+// ones: finite where the row is, and the other operand of their product is zero.
+template <typename V, typename T>
+__device__ __forceinline__ V load_at(const T* base, unsigned at) {
+  return *reinterpret_cast<const V*>(reinterpret_cast<const char*>(base) + at * (unsigned)sizeof(T));
+}
 template <typename T, int VEC>
 __device__ __forceinline__ x8_t<T> load8_within(const T* base, unsigned at, int d0, int D) {
   if constexpr (VEC == 8 && sizeof(T) == 2) {
     typedef bf16x8 any8 __attribute__((aligned(2)));
-    return *reinterpret_cast<const any8*>(base + (at + min(d0, D - 8)));
+    return load_at<any8>(base, at + min(d0, D - 8));
   } else if constexpr (VEC >= 4) {
     typedef x4_t<T> any4 __attribute__((aligned(sizeof(T))));
-    const x4_t<T> lo = *reinterpret_cast<const any4*>(base + (at + min(d0, D - 4)));
-    const x4_t<T> hi = *reinterpret_cast<const any4*>(base + (at + min(d0 + 4, D - 4)));
+    const x4_t<T> lo = load_at<any4>(base, at + min(d0, D - 4));
+    const x4_t<T> hi = load_at<any4>(base, at + min(d0 + 4, D - 4));
     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   } else {
     x8_t<T> v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = base[at + min(d0 + e, D - 1)];
+    for (int e = 0; e < 8; ++e) v[e] = load_at<T>(base, at + min(d0 + e, D - 1));
     return v;
   }
 }

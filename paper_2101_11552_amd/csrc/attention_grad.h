@@ -115,6 +115,12 @@ template <typename T, int DP, int TILES> constexpr int grad_waves() {
 // column tiles too, width 32 with a bias: 170 -> 218, a wavefront a SIMD less).
 template <typename T, int DP> constexpr bool swapped_chunks() { return sizeof(T) == 2 && DP <= 32; }
 
+// Operands in registers: the last products' column operands are read from LDS one step
+// ahead in bf16, where the compiler would wait for each pair (4 graphs of 1,500, 8 heads on
+// 4 of width 64, capped: 220 -> 174 us; of 128 with a bias 496 -> 486). float32's products
+// take longer than a read, and its operands twice the registers.
+template <typename T> constexpr int operands_ahead() { return sizeof(T) == 2 ? 2 : 1; }
+
 template <typename T, int DP, int WAVES, int QT, int VEC, bool BIAS, bool CAP, bool REST>
 __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn_grad_q(AttnGrad p) {
   // keys of a tile: as many as leave LDS for two blocks a CU beside the bias's bins
@@ -122,6 +128,7 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
   // with 64; without a bias or a cap the whole gradient takes 566 us with 64, 652 with 32)
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 && !(BIAS && DP == 128) ? 64 : 32;
   constexpr int THREADS = WAVES * kWave;
+  constexpr int NB = operands_ahead<T>();
   using Rows = Tile<T, DP, swapped_chunks<T, DP>()>;
   using Columns = Tile<T, BN, false>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
@@ -411,11 +418,22 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
           }
           sf[t] = as_operand<T>(sc[0][t], sc[1][t]);
         }
+        constexpr int AT = NB == 2 && DT >= 2 ? 2 : 1;  // column tiles of a step
+        x8_t<T> kf[NB][AT];
+        const auto operands = [&](int d) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const x8_t<T> kf = Columns::get8(Kt, d * 16 + col, x2 * 32 + g * 8);
+          for (int e = 0; e < AT; ++e) kf[d % NB][e] = Columns::get8(Kt, (d * AT + e) * 16 + col, x2 * 32 + g * 8);
+        };
+        if (NB == 2) operands(0);
 #pragma unroll
-          for (int t = 0; t < QT; ++t) o[t][d] = mma(kf, sf[t], o[t][d]);
+        for (int d = 0; d < DT / AT; ++d) {
+          if (d + NB - 1 < DT / AT) operands(d + NB - 1);
+          if (NB == 2) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int e = 0; e < AT; ++e)
+#pragma unroll
+            for (int t = 0; t < QT; ++t) o[t][d * AT + e] = mma(kf[d % NB][e], sf[t], o[t][d * AT + e]);
+          if (NB == 2) __builtin_amdgcn_sched_barrier(0);
         }
       }
       if (BIAS && kt + 1 < tiles) fetch_buckets(kt + 1);
@@ -475,9 +493,10 @@ __device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
 }
 
 template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP, bool REST>
-__global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn_grad_kv(AttnGrad p) {
+__global__ __launch_bounds__(WAVES * kWave, sizeof(T) == 2 && DP == 64 && VEC == 8 && !BIAS && !REST ? 3 : grad_waves<T, DP, KT>()) void attn_grad_kv(AttnGrad p) {
   constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave;
+  constexpr int NB = operands_ahead<T>();
   using Rows = Tile<T, DP, swapped_chunks<T, DP>()>;
   using Columns = Tile<T, BR, false>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, XT = BR / 16;
@@ -664,15 +683,22 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn
           pf[t] = as_operand<T>(sc[t][0], sc[t][1]);
           sf[t] = as_operand<T>(dp[t][0], dp[t][1]);
         }
+        x8_t<T> of[NB], qf[NB];
+        const auto operands = [&](int d) {
+          of[d % NB] = Columns::get8(Ot, d * 16 + col, x2 * 32 + g * 8);
+          qf[d % NB] = Columns::get8(Qt, d * 16 + col, x2 * 32 + g * 8);
+        };
+        if (NB == 2) operands(0);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const x8_t<T> of = Columns::get8(Ot, d * 16 + col, x2 * 32 + g * 8);
-          const x8_t<T> qf = Columns::get8(Qt, d * 16 + col, x2 * 32 + g * 8);
+          if (d + NB - 1 < DT) operands(d + NB - 1);
+          if (NB == 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
           for (int t = 0; t < KT; ++t) {
-            dv[t][d] = mma(of, pf[t], dv[t][d]);
-            dk[t][d] = mma(qf, sf[t], dk[t][d]);
+            dv[t][d] = mma(of[d % NB], pf[t], dv[t][d]);
+            dk[t][d] = mma(qf[d % NB], sf[t], dk[t][d]);
           }
+          if (NB == 2) __builtin_amdgcn_sched_barrier(0);
         }
       }
       if (BIAS && it + 1 < total) fetch_buckets(it + 1);
