@@ -493,7 +493,7 @@ __device__ __forceinline__ unsigned transpose_quad(unsigned v, unsigned j) {
 }
 
 template <typename T, int DP, int WAVES, int KT, int VEC, bool BIAS, bool CAP, bool REST>
-__global__ __launch_bounds__(WAVES * kWave, sizeof(T) == 2 && DP == 64 && VEC == 8 && !BIAS && !REST ? 3 : grad_waves<T, DP, KT>()) void attn_grad_kv(AttnGrad p) {
+__global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, KT>())) void attn_grad_kv(AttnGrad p) {
   constexpr int BK = WAVES * KT * 16, BR = sizeof(T) == 2 ? 64 : 32;
   constexpr int THREADS = WAVES * kWave;
   constexpr int NB = operands_ahead<T>();
