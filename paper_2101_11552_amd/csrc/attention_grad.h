@@ -115,6 +115,13 @@ template <typename T, int DP, int TILES> constexpr int grad_waves() {
 // column tiles too, width 32 with a bias: 170 -> 218, a wavefront a SIMD less).
 template <typename T, int DP> constexpr bool swapped_chunks() { return sizeof(T) == 2 && DP <= 32; }
 
+// bf16 heads of up to 32 columns: ds as two operands, its rounding and what that left over.
+// A row's ds add up to zero, so its dq is what few terms leave of larger ones: with ds
+// rounded once and delta from the rounded output, dq of width 8 was off by 2.7e-3 of its
+// norm (of wide heads 2.4e-3, of its own rounding alone 1.7e-3). One product more: 160 ->
+// 164 us with a bias, 4 graphs of 1,500, 8 heads on 4.
+template <typename T, int DP> constexpr bool splits_ds() { return sizeof(T) == 2 && DP <= 32; }
+
 // Operands in registers: the last products' column operands are read from LDS one step
 // ahead in bf16, where the compiler would wait for each pair (4 graphs of 1,500, 8 heads on
 // 4 of width 64, capped: 220 -> 174 us; of 128 with a bias 496 -> 486). float32's products
@@ -129,6 +136,7 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
   constexpr int BM = WAVES * QT * 16, BN = sizeof(T) == 2 && !(BIAS && DP == 128) ? 64 : 32;
   constexpr int THREADS = WAVES * kWave;
   constexpr int NB = operands_ahead<T>();
+  constexpr bool SPLIT = splits_ds<T, DP>();
   using Rows = Tile<T, DP, swapped_chunks<T, DP>()>;
   using Columns = Tile<T, BN, false>;
   constexpr int KC = Frag<T, DP>::KC, DT = DP / 16, KT = BN / 16;
@@ -387,7 +395,7 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
         f32x4 sc[2][QT], dp[2][QT];
         products(2 * x2, sc[0], dp[0]);
         products(2 * x2 + 1, sc[1], dp[1]);
-        x8_t<T> sf[QT];
+        x8_t<T> sf[QT], lo[QT];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           const float* th = tab + hg[t] * (a.B + 1);
@@ -417,6 +425,14 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
             add_to_bins(bin, b[1], dp[1][t]);
           }
           sf[t] = as_operand<T>(sc[0][t], sc[1][t]);
+          if (SPLIT) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              sc[0][t][i] -= (float)sf[t][i];
+              sc[1][t][i] -= (float)sf[t][4 + i];
+            }
+            lo[t] = as_operand<T>(sc[0][t], sc[1][t]);
+          }
         }
         constexpr int AT = NB == 2 && DT >= 2 ? 2 : 1;  // column tiles of a step
         x8_t<T> kf[NB][AT];
@@ -432,7 +448,10 @@ __global__ __launch_bounds__(WAVES * kWave, (grad_waves<T, DP, QT>())) void attn
 #pragma unroll
           for (int e = 0; e < AT; ++e)
 #pragma unroll
-            for (int t = 0; t < QT; ++t) o[t][d * AT + e] = mma(kf[d % NB][e], sf[t], o[t][d * AT + e]);
+            for (int t = 0; t < QT; ++t) {
+              if (SPLIT) o[t][d * AT + e] = mma(kf[d % NB][e], lo[t], o[t][d * AT + e]);
+              o[t][d * AT + e] = mma(kf[d % NB][e], sf[t], o[t][d * AT + e]);
+            }
           if (NB == 2) __builtin_amdgcn_sched_barrier(0);
         }
       }
