@@ -19,7 +19,7 @@ int launch_fwd_rows(AttnFwd& p, hipStream_t s) {
   p.heads = 1;
   p.small = 0;
   const bool whole = whole_vectors<T>(D);
-  if (p.nsplit == 1 && whole && small_graphs(p.a.Nq, p.a.Nk, p.a.G, p.a.Hk)) {
+  if (p.nsplit == 1 && whole && small_graphs(p.a.Nq, p.a.Nk, p.a.G, p.a.Hk) && small_fits<T, DP>(p.a)) {
     if (int rc = launch_small<T, DP>(p, s)) return rc;
     p.small = kSmallGraph;  // the rest: graphs with more nodes, few if any
     p.heads = p.a.Hk;

@@ -207,10 +207,17 @@ inline int small_waves(const AttnShape& a, int per_cu) {
   return (int)(std::min<int64_t>(a.G, most) * a.Hk);
 }
 
+// Bytes of LDS a wavefront takes; a block of four has to fit a CU.
+template <typename T, int DP> size_t small_lds_bytes(const AttnShape& a) {
+  return (bias_table_bytes(a) + 15) / 16 * 16 + sizeof(T) * small_fwd_lds<T, DP>();
+}
+template <typename T, int DP> bool small_fits(const AttnShape& a) {
+  return 4 * small_lds_bytes<T, DP>(a) <= size_t(160) << 10;
+}
+
 template <typename T, int DP>
 int launch_small(const AttnFwd& p, hipStream_t s) {
-  const int tabn = p.a.B > 0 ? (int)((bias_table_bytes(p.a) / 4 + 3) / 4 * 4) : 0;
-  const size_t lds = sizeof(float) * tabn + sizeof(T) * small_fwd_lds<T, DP>();
+  const size_t lds = small_lds_bytes<T, DP>(p.a);
   const int waves = small_waves(p.a, 16);
   const unsigned blocks = (unsigned)((waves + 3) / 4);
   const int cap = p.a.cap <= 0.0f ? 0 : p.a.B > 0 || p.a.cap > kBoundedCap ? 1 : 2;

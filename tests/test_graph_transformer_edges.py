@@ -119,6 +119,17 @@ def test_attention_nothing(tfg, name, sizes):
     torch.cuda.synchronize()
 
 
+def test_attention_large_bias_tables(tfg):
+    """Many small graphs whose heads' bias tables leave no room for a wavefront a graph."""
+    c = Case("f32", SIZES["many"], 64, 4, 128, 0.0, 255, seed=115)
+    out, lse = c.forward(tfg)
+    ref = c.reference()
+    within(out, ref["out"], ref["t_out"] + 1e-37, "out")
+    dq, dk, dv, dbias = c.backward(tfg, out, lse)
+    for x, key in ((dq, "dq"), (dk, "dk"), (dv, "dv"), (dbias, "dbias")):
+        within(x, ref[key], ref["t_" + key] + 1e-37, key)
+
+
 def test_group_norm_nothing(tfg):
     import torch
     x = normal(120, 0, 16)
