@@ -637,6 +637,8 @@ int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int
  * share them), dbias NULL or [H, B]. The softmax's weights are formed again from
  * lse. bf16: the weights and their gradients are rounded to bf16 as operands of the
  * products, sums are float32.
+ * A non-finite value in q, k, v or dout reaches the gradients of its whole graph and of the
+ * heads that share it, masked or not, and no other graph's.
  */
 size_t tfg_graph_attention_ws_bytes(int64_t Nq, int64_t Nk, int64_t G, int64_t H, int64_t kv_heads,
                                     int64_t D);

@@ -11,6 +11,8 @@
 // every run that lies inside it; a run that crosses a tile's edge leaves float32
 // partial rows, which a second kernel joins in tile order. Rows without ids get
 // zeros. No atomics: the order of every sum is fixed by the ids.
+//
+// What bounds it: memory, and for the gradient the sort's launches before it (ZIPF).
 #include "rows.h"
 
 namespace tfg {
