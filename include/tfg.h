@@ -613,7 +613,8 @@ int tfg_group_norm_backward(const void *dout, const void *x, int float_type, int
  * tfg_batch_graphs writes its node offsets; self-attention passes one array
  * twice, a readout a few queries per graph). For query i, key j of one graph and
  * head h, whose key/value head is h / (H / kv_heads):
- *   s = scale * <q[i, h], k[j]>,  t = cap * tanh(s / cap)  (cap = 0: t = s),
+ *   s = scale * <q[i, h], k[j]>,  t = cap * tanh(s / cap)  (cap = 0: t = s; bf16: at most
+ *   4096, t within 2^-20 cap),
  *   u = t + bias[h, d_ij],
  *   out[i, h] = sum over j of softmax_j(u) * v[j]
  * bias: NULL (B = 0), or [H, B] of the features' type, B <= 255, with distance the

@@ -1009,6 +1009,10 @@ int check_attention(const AttnShape& a, int float_type, int64_t Nq, int64_t Nk, 
   if (a.ldq >= (int64_t(1) << 23) || a.ldk >= (int64_t(1) << 23) || a.ldv >= (int64_t(1) << 23))
     return fail(TFG_ERR_TOO_LARGE, "a leading dimension not below 2^23");
   if (!(a.cap >= 0.0f) || a.cap > 3.4e38f) return fail(TFG_ERR_INVALID_ARG, "bad cap");
+  if (float_type == TFG_BF16 && a.cap > 4096.0f)  // (its tanh is exact to 2^-21 of the cap)
+    return fail(TFG_ERR_INVALID_ARG, "a cap above 4096 for bfloat16 (0: none)");
+  if (a.cap > 0.0f && (a.scale > a.cap * 1e37f || a.scale < a.cap * -1e37f))
+    return fail(TFG_ERR_INVALID_ARG, "scale / cap overflows");
   if (B < 0 || B > 255) return fail(TFG_ERR_INVALID_ARG, "need 0 <= B <= 255");
   if (H / Hk * B > max_attention_bias_entries())
     return fail(TFG_ERR_INVALID_ARG, "need H / kv_heads * B <= 4096");

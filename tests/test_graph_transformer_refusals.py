@@ -143,3 +143,14 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         tfg.tfg_graph_attention(x, x, x, off, 2)
     with pytest.raises(ValueError):
         tfg.tfg_graph_attention_backward(x, x, x, x, x, x, off, 2)
+
+
+@pytest.mark.parametrize("call", [attention, attention_backward])
+def test_attention_cap_refusals(lib, call):
+    """A cap whose tanh bfloat16's form would not resolve, and one that scale / cap overflows."""
+    assert call(lib, ft=1, cap=4097.0) == INVALID
+    assert call(lib, cap=1e-38) == INVALID and call(lib, ft=1, cap=1e-39) == INVALID
+    # (with a workspace too small: the next check is reached)
+    assert call(lib, ft=1, cap=4096.0, n=8) == WORKSPACE
+    assert call(lib, ft=0, cap=1e30, n=8) == WORKSPACE
+    assert call(lib, cap=1e-30, n=8) == WORKSPACE
